@@ -298,6 +298,96 @@ rocs_status_t rocs_linear_normed(rocs_dtype_t dtype, rocs_norm_t kind, int64_t M
                                  void* stream);
 
 /*
+ * Paged cache of request histories: the keys and values of a request's sequence (Eq. 13: once per request, Section
+ * 4.3.1) kept between its visits, in pages that several slots may hold together.
+ *   K, V    pages: element (layer, id, i, h, c) at layer * ld_layer + id * ld_page + i * ld_token + h * ld_head + c,
+ *           id < n_pages, i < page, h < H_kv, c < dh; both with the same strides (elements, of 16-byte multiples;
+ *           any order of the dimensions, e.g. [layers, n_pages, page, H_kv, dh] or [layers, n_pages, H_kv, page, dh])
+ *   table   [n_slots, width] int32: position j of slot s is row j % page of page table[s, j / page]
+ *   lens    [n_slots] int32: positions that a slot holds
+ *   refs    [n_pages] int32: slots that hold a page, 0 = free; NULL where the caller keeps pages itself (then only
+ *           rocs_cache_append and rocs_cache_attention apply)
+ * A cache names these arrays (16-byte aligned, device memory of the caller, who may read and write them in stream
+ * order) and owns no device memory; creating and destroying it enqueues nothing.  Lengths outside 0..width * page count
+ * as the nearer end.  An entry of the table outside 0..n_pages-1 reads as a page of zeros and is never written through.
+ * Limits: width <= 2^20, width * page and page * H_kv * dh < 2^31, dh <= 256, dh * sizeof(element) a multiple of 16.
+ *
+ * The calls that keep the books (extend, fork, truncate, compact) run on the device without the host: no
+ * synchronisation, and a captured one works on what it finds at each replay.  They are all or nothing: a call that
+ * cannot be carried out changes nothing and says so in `report` (device int32 [2], may be NULL): [0] 0 = done,
+ * 1 = too few free pages, 2 = a slot out of range or named twice, 3 = a slot would outgrow its row of the table or has a
+ * length outside it, 4 = a child that is not empty, 5 = a page id outside the pool; [1] pages taken / shared / given
+ * back / in use (extend / fork / truncate / compact; for 1 how many are missing).  `workspace`: rocs_cache_workspace
+ * bytes for the largest number of slots of a call, 256-byte aligned, contents overwritten.
+ * Errors of all: INVALID_ARG, ALIGNMENT, WORKSPACE, UNSUPPORTED, CUDA.
+ */
+typedef struct rocs_cache rocs_cache_t; /* opaque; owned by the library */
+rocs_status_t rocs_cache_create(rocs_cache_t** out, rocs_dtype_t dtype, int32_t layers, int32_t n_pages, int32_t page,
+                                int32_t H_kv, int32_t dh, void* K, void* V, int64_t ld_layer, int64_t ld_page,
+                                int64_t ld_token, int64_t ld_head, int32_t n_slots, int32_t width, int32_t* table,
+                                int32_t* lens, int32_t* refs);
+rocs_status_t rocs_cache_destroy(rocs_cache_t* cache);
+size_t rocs_cache_workspace(const rocs_cache_t* cache, int32_t n);
+
+/*
+ * Room for the batch's new rows: request r of `plan` (its rows are the new positions) grows slot slots[r] (device
+ * int32 [R]; NULL: slot r) by n_r.  Pages come from the free ones, lowest index first, in order of request and
+ * position.  A last page that is partly filled and held by others too is replaced by a copy of itself (all layers),
+ * where n_r > 0; two requests that share it get a copy each.  first [R] receives the position of each request's first
+ * new row, -1 if the call was not carried out.
+ */
+rocs_status_t rocs_cache_extend(const rocs_cache_t* cache, const rocs_plan_t* plan, const int32_t* slots, int32_t* first,
+                                int32_t* report, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Writes the new rows of one layer: row i of request r, the t-th of it, goes to position first[r] + t of its slot.
+ * Nothing is written where first[r] < 0 or past the slot's row of the table.  No two requests may write the same
+ * position.
+ *   K_new, V_new [N, H_kv, dh] with strides ld_token, ld_head (elements, of 16-byte multiples)
+ */
+rocs_status_t rocs_cache_append(const rocs_cache_t* cache, int32_t layer, const rocs_plan_t* plan, const int32_t* slots,
+                                const int32_t* first, const void* K_new, const void* V_new, int64_t ld_token,
+                                int64_t ld_head, void* stream);
+
+/* children[i] (empty) becomes a copy of parents[i] that shares its pages, for i < n (device int32 [n]). */
+rocs_status_t rocs_cache_fork(const rocs_cache_t* cache, int32_t n, const int32_t* parents, const int32_t* children,
+                              int32_t* report, void* workspace, size_t workspace_bytes, void* stream);
+
+/* Slot slots[i] keeps its first keep[i] positions (keep NULL: none); pages behind them are given back. */
+rocs_status_t rocs_cache_truncate(const rocs_cache_t* cache, int32_t n, const int32_t* slots, const int32_t* keep,
+                                  int32_t* report, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Moves the pages in use, in order, so that they are the first ones of the pool: those behind the line go to the free
+ * ones in front of it, in all layers.  table_out [n_slots, width] and refs_out [n_pages] receive the new table and
+ * holders (NULL: in place).  No page in use is overwritten, so readers of the old table may go on with it.
+ */
+rocs_status_t rocs_cache_compact(const rocs_cache_t* cache, int32_t* table_out, int32_t* refs_out, int32_t* report,
+                                 void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Attention of the batch's rows over their slots of the cache (Eq. 13 with K/V in pages).  Request r of `plan` owns n_r
+ * query rows and reads slot slots[r] (NULL: slot r; out of range: an empty one) with its L = lens[slot] positions.
+ *   causal != 0: the rows are the slot's last n_r positions (a chunk of new events, already appended; n_r = 1: one
+ *                event); row t stands at p = L - n_r + t and sees the keys j < max(p + 1, prefix[r])
+ *   causal == 0: the rows are candidates; each stands at p = L and sees all L keys (prefix must be NULL)
+ *   begin [N] int32 or NULL: row i sees no key in front of begin[i] (the start of its session or document)
+ *   prefix [R] int32 or NULL: keys in front of prefix[r] are visible to all of r's rows
+ *   score  x_j = scale <q, k_j>, scale <= 0: 1/sqrt(dh);  cap > 0: x_j = cap tanh(x_j / cap);  slopes [H] fp32 or NULL:
+ *          x_j - slopes[h] |p - j|
+ *   O[i, h, :] = sum_j softmax_j(x) V_j over the visible j, zeros where none is.  H query heads, a multiple of the cache's
+ *   H_kv: head h reads key head h / (H / H_kv).
+ *   Q [N, H, dh], ld_qt, ld_qh and O [N, H, dh], ld_ot, ld_oh: strides of row and head (elements, of 16-byte multiples)
+ * Keys that a row does not see have no influence on it, whatever they hold (NaN and Inf included).
+ *   workspace >= rocs_cache_attention_workspace(cache, plan, H) bytes, 256-byte aligned; contents are overwritten
+ */
+size_t rocs_cache_attention_workspace(const rocs_cache_t* cache, const rocs_plan_t* plan, int32_t H);
+rocs_status_t rocs_cache_attention(const rocs_cache_t* cache, int32_t layer, const rocs_plan_t* plan, const int32_t* slots,
+                                   int32_t H, const void* Q, int64_t ld_qt, int64_t ld_qh, int32_t causal, float scale,
+                                   float cap, const float* slopes, const int32_t* begin, const int32_t* prefix, void* O,
+                                   int64_t ld_ot, int64_t ld_oh, void* workspace, size_t workspace_bytes, void* stream);
+
+/*
  * Device-side status of the tensor-core kernels.  Their barrier waits are bounded; a wait
  * that expires records a code in a device word instead of spinning forever and the kernel
  * returns.  This call synchronises the device, reads the word, clears it and returns

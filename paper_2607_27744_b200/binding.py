@@ -6,7 +6,8 @@ library is missing or a call fails, an exception is raised.  The calls of a scor
 the extension ``_native`` (``csrc/binding.cpp``), the rest through ctypes.
 
 Functions mirror the C entry points (``rocs_`` prefix dropped): :func:`plan_create`,
-:func:`ikbo_linear`, :func:`linear`, :func:`dca_attention`, :func:`glm_interaction`.
+:func:`ikbo_linear`, :func:`linear`, :func:`dca_attention`, :func:`glm_interaction`, :func:`cache_create`,
+:func:`cache_attention`.
 bf16 tensors are ``torch.bfloat16``, fp32 tensors ``torch.float32``.
 """
 from __future__ import annotations
@@ -35,7 +36,9 @@ EXPORTS = [
     "rocs_glm_fm_projection_workspace", "rocs_glm_fm_projection", "rocs_group_norm",
     "rocs_last_device_status", "rocs_ikbo_linear_static", "rocs_ikbo_linear_static_max_z_elems",
     "rocs_ikbo_linear_static_max_candidates", "rocs_ikbo_linear_stats_workspace", "rocs_ikbo_linear_stats",
-    "rocs_weight_row_sums", "rocs_linear_normed",
+    "rocs_weight_row_sums", "rocs_linear_normed", "rocs_cache_create", "rocs_cache_destroy", "rocs_cache_workspace",
+    "rocs_cache_extend", "rocs_cache_append", "rocs_cache_fork", "rocs_cache_truncate", "rocs_cache_compact",
+    "rocs_cache_attention_workspace", "rocs_cache_attention",
 ]
 
 
@@ -275,3 +278,88 @@ def ikbo_linear_static(cand_offsets: torch.Tensor, XR: torch.Tensor, XC: torch.T
     output tensor; scratch lives in a fixed array inside the library (limits: R * d_out <= 1 Mi,
     N <= 256 Ki; calls share the array, so do not let two of them overlap on the GPU)."""
     return (_ext or _native()).ikbo_linear_static(cand_offsets, XR, XC, W_CR, W_CC, out, bias, relu)
+
+
+class Cache:
+    """Owns a ``rocs_cache_t``: names the pages, table, lengths and holders of a paged cache of request histories and keeps
+    these tensors alive; the caller may read and write them in stream order."""
+
+    def __init__(self, K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                 refs: Optional[torch.Tensor] = None):
+        self.spec = None
+        if K.dim() == 4:
+            K, V = K.unsqueeze(0), V.unsqueeze(0)
+        self.K, self.V, self.table, self.lens, self.refs = K, V, table, lens, refs
+        self.spec = (_ext or _native()).cache_create(K, V, table, lens, refs)
+
+    def close(self):
+        spec, self.spec = self.spec, None
+        if spec:
+            _ext.cache_destroy(spec[0])
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+def cache_create(K: torch.Tensor, V: torch.Tensor, table: torch.Tensor, lens: torch.Tensor,
+                 refs: Optional[torch.Tensor] = None) -> Cache:
+    """A paged cache over K, V [layers, n_pages, page, H_kv, dh] (or without layers; any strides, the same for both, last
+    dimension contiguous), table [n_slots, width], lens [n_slots], refs [n_pages], all int32.  refs=None: the caller keeps
+    the pages itself and only appends and attends."""
+    return Cache(K, V, table, lens, refs)
+
+
+def cache_workspace(cache: Cache, n: int) -> int:
+    """Bytes of workspace that the bookkeeping calls on up to n slots take."""
+    return (_ext or _native()).cache_workspace(cache.spec, n)
+
+
+def cache_extend(cache: Cache, plan: Plan, slots: Optional[torch.Tensor] = None, report: Optional[torch.Tensor] = None,
+                 first: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Room for each request's new rows in its slot; a partly filled last page that is shared becomes a copy first.
+    Returns the position of each request's first new row, -1 where the call could not be carried out (see ``report``)."""
+    return (_ext or _native()).cache_extend(cache.spec, plan.handle, plan.R, plan.N, slots, first, report, workspace)
+
+
+def cache_append(cache: Cache, plan: Plan, first: torch.Tensor, K_new: torch.Tensor, V_new: torch.Tensor,
+                 slots: Optional[torch.Tensor] = None, layer: int = 0) -> None:
+    """Writes the new rows K_new, V_new [N, H_kv, dh] of one layer from position first[r] of each request's slot on."""
+    (_ext or _native()).cache_append(cache.spec, plan.handle, plan.R, plan.N, first, K_new, V_new, slots, layer)
+
+
+def cache_fork(cache: Cache, parents: torch.Tensor, children: torch.Tensor, report: Optional[torch.Tensor] = None,
+               workspace: Optional[torch.Tensor] = None) -> None:
+    """The empty slots children become copies of parents that share their pages."""
+    (_ext or _native()).cache_fork(cache.spec, parents, children, report, workspace)
+
+
+def cache_truncate(cache: Cache, slots: torch.Tensor, keep: Optional[torch.Tensor] = None, report: Optional[torch.Tensor] = None,
+                   workspace: Optional[torch.Tensor] = None) -> None:
+    """Each slot keeps its first keep[i] positions (none by default); the pages behind are given back."""
+    (_ext or _native()).cache_truncate(cache.spec, slots, keep, report, workspace)
+
+
+def cache_compact(cache: Cache, table_out: Optional[torch.Tensor] = None, refs_out: Optional[torch.Tensor] = None,
+                  report: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> None:
+    """Moves the pages in use to the front of the pool; the new table and holders go to table_out and refs_out, in place
+    by default."""
+    (_ext or _native()).cache_compact(cache.spec, table_out, refs_out, report, workspace)
+
+
+def cache_attention_workspace(cache: Cache, plan: Plan, H: int) -> int:
+    return (_ext or _native()).cache_attention_workspace(cache.spec, plan.handle, plan.R, plan.N, H)
+
+
+def cache_attention(cache: Cache, plan: Plan, Q: torch.Tensor, slots: Optional[torch.Tensor] = None, layer: int = 0,
+                    causal: bool = True, scale: float = 0.0, cap: float = 0.0, slopes: Optional[torch.Tensor] = None,
+                    begin: Optional[torch.Tensor] = None, prefix: Optional[torch.Tensor] = None,
+                    out: Optional[torch.Tensor] = None, workspace: Optional[torch.Tensor] = None) -> torch.Tensor:
+    """Attention of each request's rows Q [N, H, dh] over its slot of the cache (Eq. 13 with K/V in pages): a chunk of new
+    events (causal; they are the slot's last positions) or the request's candidates (causal=False: all keys).
+    cap: scores become cap tanh(score / cap); slopes [H]: minus slope times distance; begin [N]: the first key a row sees;
+    prefix [R]: keys in front of it are visible to all of a request's rows."""
+    return (_ext or _native()).cache_attention(cache.spec, plan.handle, plan.R, plan.N, Q, slots, layer, causal, scale, cap, slopes,
+                                               begin, prefix, out, workspace)

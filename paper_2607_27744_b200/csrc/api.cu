@@ -6,6 +6,7 @@
 #include <mutex>
 #include <new>
 
+#include "cache.h"
 #include "rocs_internal.h"
 #include "sm100_ptx.cuh"
 
@@ -79,6 +80,8 @@ static cudaError_t pool_alloc(void** ptr, size_t bytes, cudaStream_t stream) {
   }
   return cudaMallocFromPoolAsync(ptr, bytes, pool, stream);
 }
+
+int kernel_path() { return g_path.load(); }
 
 uint32_t* device_status_word() {
   uint32_t* p = nullptr;
@@ -467,6 +470,7 @@ rocs_status_t rocs_plan_create(rocs_plan_t** out, int32_t R, int64_t N, const in
     delete p;
     return ROCS_ERR_SEGMENTS;
   }
+  for (int32_t r = 0; r < R; ++r) p->largest = std::max(p->largest, off[r + 1] - off[r]);
   if (cudaGetDevice(&p->device) != cudaSuccess) {
     delete p;
     return ROCS_ERR_CUDA;

@@ -9,6 +9,7 @@
 #include <Python.h>
 
 #include <ATen/ops/empty.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -368,6 +369,237 @@ PyObject* ikbo_linear_static(PyObject* const* a) {
   return Py_NewRef(a[5]);
 }
 
+// ---- the paged cache ----------------------------------------------------------------------------------
+// What binding.Cache keeps of a handle: (handle, device, dtype, layers, n_slots, width, n_pages, H_kv, dh).
+struct CacheArg {
+  const rocs_cache_t* handle;
+  int64_t v[8];
+  explicit CacheArg(PyObject* o) : handle(nullptr) {
+    if (!PyTuple_Check(o) || PyTuple_GET_SIZE(o) != 9) raise(PyExc_ValueError, "the cache is closed");
+    handle = static_cast<const rocs_cache_t*>(PyLong_AsVoidPtr(PyTuple_GET_ITEM(o, 0)));
+    for (int i = 0; i < 8; ++i) v[i] = PyLong_AsLongLong(PyTuple_GET_ITEM(o, i + 1));
+    if (PyErr_Occurred()) throw PyRaised{};
+    require(v[0] == c10::cuda::current_device(), "the cache is on another device than the current one");
+  }
+  int64_t device() const { return v[0]; }
+  at::ScalarType dtype() const { return v[1] == ROCS_BF16 ? at::kBFloat16 : at::kFloat; }
+  int64_t n_slots() const { return v[3]; }
+  int64_t width() const { return v[4]; }
+  int64_t n_pages() const { return v[5]; }
+  int64_t heads() const { return v[6]; }
+  int64_t dh() const { return v[7]; }
+  // a tensor of the cache's device, of a type
+  void same(const Arg& t, at::ScalarType type, const char* what) const {
+    require(t->is_cuda() && t->get_device() == device() && t->scalar_type() == type, what);
+  }
+  const int32_t* ints(const Arg& t, int64_t n, const char* what) const {
+    if (!t) return nullptr;
+    same(t, at::kInt, what);
+    require(t->is_contiguous() && t->numel() == n, what);
+    return static_cast<const int32_t*>(t.ptr());
+  }
+  // rows [N, heads, dh] with a contiguous last dimension
+  void rows(const Arg& t, int64_t N, int64_t H, const char* what) const {
+    t.need_dims(3);
+    same(t, dtype(), what);
+    require(t->size(0) == N && t->size(1) == H && t->size(2) == dh() && (dh() == 1 || t->stride(2) == 1), what);
+  }
+  at::Tensor bytes(size_t n) const {
+    return at::empty({(int64_t)n}, at::TensorOptions().dtype(at::kByte).device(at::kCUDA, (c10::DeviceIndex)device()));
+  }
+};
+struct Workspace {
+  at::Tensor made;
+  void* ptr;
+  size_t size;
+  Workspace(const Arg& given, const CacheArg& c, size_t need) {
+    if (given) {
+      c.same(given, at::kByte, "workspace: a uint8 tensor of the cache's device");
+      require(given->is_contiguous(), "workspace: contiguous");
+      ptr = given.mut();
+      size = given.bytes();
+    } else {
+      made = c.bytes(need);
+      ptr = made.mutable_data_ptr();
+      size = need;
+    }
+  }
+};
+int64_t stride_of(const Arg& t, int64_t d, int64_t least) { return t->size(d) > 1 ? t->stride(d) : least; }
+
+// K, V, table, lens, refs -> what CacheArg takes
+PyObject* cache_create(PyObject* const* a) {
+  const Arg K(a[0]), V(a[1]), table(a[2]), lens(a[3]), refs(a[4]);
+  K.need_dims(5);
+  V.need_dims(5);
+  const rocs_dtype_t dt = K.dtype();
+  require(V->scalar_type() == K->scalar_type() && V->sizes() == K->sizes(), "K and V: the same type and sizes");
+  for (int64_t d = 0; d < 5; ++d) require(K->size(d) <= 1 || K->stride(d) == V->stride(d), "K and V: the same strides");
+  require(K->size(4) <= 1 || K->stride(4) == 1, "K and V: a contiguous last dimension");
+  table.need_dims(2);
+  lens.need_dims(1);
+  for (const Arg* t : {&K, &V, &table, &lens, &refs})
+    if (*t) require((*t)->is_cuda() && (*t)->get_device() == c10::cuda::current_device(), "tensors of the current device");
+  for (const Arg* t : {&table, &lens, &refs})
+    if (*t) require((*t)->scalar_type() == at::kInt && (*t)->is_contiguous(), "table, lens, refs: contiguous int32");
+  require(lens->size(0) == table->size(0), "lens: one per row of the table");
+  if (refs) require(refs->dim() == 1 && refs->size(0) == K->size(1), "refs: one per page");
+  for (int64_t d = 0; d < 5; ++d) require(K->size(d) <= 0x7fffffff, "sizes below 2^31");
+  rocs_cache_t* c = nullptr;
+  check(rocs_cache_create(&c, dt, (int32_t)K->size(0), (int32_t)K->size(1), (int32_t)K->size(2), (int32_t)K->size(3),
+                          (int32_t)K->size(4), K.mut(), V.mut(), K->stride(0), K->stride(1), K->stride(2), K->stride(3),
+                          (int32_t)table->size(0), (int32_t)table->size(1), static_cast<int32_t*>(table.mut()),
+                          static_cast<int32_t*>(lens.mut()), static_cast<int32_t*>(refs.mut())),
+        "rocs_cache_create");
+  return Py_BuildValue("NiiLLLLLL", PyLong_FromVoidPtr(c), (int)K->get_device(), (int)dt, (long long)K->size(0),
+                       (long long)table->size(0), (long long)table->size(1), (long long)K->size(1), (long long)K->size(3),
+                       (long long)K->size(4));
+}
+
+PyObject* cache_destroy(PyObject* const* a) {
+  rocs_cache_destroy(static_cast<rocs_cache_t*>(PyLong_AsVoidPtr(a[0])));
+  Py_RETURN_NONE;
+}
+
+// cache, n
+PyObject* cache_workspace(PyObject* const* a) {
+  const CacheArg c(a[0]);
+  return PyLong_FromSize_t(rocs_cache_workspace(c.handle, i32(a[1])));
+}
+
+// cache, plan (3), slots, first, report, workspace
+PyObject* cache_extend(PyObject* const* a) {
+  const CacheArg c(a[0]);
+  const PlanArg plan(a + 1);
+  const Arg slots(a[4]), report(a[6]), ws(a[7]);
+  Out first(a[5]);
+  if (!first.given) {
+    first.made = at::empty({plan.R}, at::TensorOptions().dtype(at::kInt).device(at::kCUDA, (c10::DeviceIndex)c.device()));
+    first.given.t = &first.made;
+  }
+  const int32_t* sl = c.ints(slots, plan.R, "slots: contiguous int32, one per request");
+  c.ints(first.given, plan.R, "first: contiguous int32, one per request");
+  c.ints(report, 2, "report: contiguous int32 [2]");
+  const Workspace w(ws, c, ws ? 0 : rocs_cache_workspace(c.handle, (int32_t)plan.R));
+  void* st = stream();
+  check(call([&] {
+          return rocs_cache_extend(c.handle, plan.handle, sl, static_cast<int32_t*>(first.given.mut()),
+                                   static_cast<int32_t*>(report.mut()), w.ptr, w.size, st);
+        }),
+        "rocs_cache_extend");
+  return first.release();
+}
+
+// cache, plan (3), first, K_new, V_new, slots, layer
+PyObject* cache_append(PyObject* const* a) {
+  const CacheArg c(a[0]);
+  const PlanArg plan(a + 1);
+  const Arg first(a[4]), K(a[5]), V(a[6]), slots(a[7]);
+  const char* what = "K_new, V_new: [N, H_kv, dh] of the cache's type and device, contiguous last dimension, the same strides";
+  c.rows(K, plan.N, c.heads(), what);
+  c.rows(V, plan.N, c.heads(), what);
+  const int64_t ld_h = stride_of(K, 1, c.dh()), ld_t = stride_of(K, 0, c.heads() * c.dh());
+  require(stride_of(V, 1, c.dh()) == ld_h && stride_of(V, 0, c.heads() * c.dh()) == ld_t, what);
+  require((bool)first, "first: what cache_extend returned");
+  const int32_t* f = c.ints(first, plan.R, "first: contiguous int32, one per request");
+  const int32_t* sl = c.ints(slots, plan.R, "slots: contiguous int32, one per request");
+  const int32_t layer = i32(a[8]);
+  void* st = stream();
+  check(call([&] { return rocs_cache_append(c.handle, layer, plan.handle, sl, f, K.ptr(), V.ptr(), ld_t, ld_h, st); }),
+        "rocs_cache_append");
+  Py_RETURN_NONE;
+}
+
+// cache, parents, children, report, workspace
+PyObject* cache_fork(PyObject* const* a) {
+  const CacheArg c(a[0]);
+  const Arg parents(a[1]), children(a[2]), report(a[3]), ws(a[4]);
+  const int64_t n = children->numel();
+  require(n <= 0x7fffffff && parents->numel() == n, "as many parents as children");
+  const int32_t* from = c.ints(parents, n, "parents: contiguous int32");
+  const int32_t* to = c.ints(children, n, "children: contiguous int32");
+  c.ints(report, 2, "report: contiguous int32 [2]");
+  const Workspace w(ws, c, ws ? 0 : rocs_cache_workspace(c.handle, (int32_t)n));
+  void* st = stream();
+  check(call([&] { return rocs_cache_fork(c.handle, (int32_t)n, from, to, static_cast<int32_t*>(report.mut()), w.ptr, w.size, st); }),
+        "rocs_cache_fork");
+  Py_RETURN_NONE;
+}
+
+// cache, slots, keep, report, workspace
+PyObject* cache_truncate(PyObject* const* a) {
+  const CacheArg c(a[0]);
+  const Arg slots(a[1]), keep(a[2]), report(a[3]), ws(a[4]);
+  const int64_t n = slots->numel();
+  require(n <= 0x7fffffff, "slots: fewer than 2^31");
+  const int32_t* sl = c.ints(slots, n, "slots: contiguous int32");
+  const int32_t* kp = c.ints(keep, n, "keep: contiguous int32, one per slot");
+  c.ints(report, 2, "report: contiguous int32 [2]");
+  const Workspace w(ws, c, ws ? 0 : rocs_cache_workspace(c.handle, (int32_t)n));
+  void* st = stream();
+  check(call([&] { return rocs_cache_truncate(c.handle, (int32_t)n, sl, kp, static_cast<int32_t*>(report.mut()), w.ptr, w.size, st); }),
+        "rocs_cache_truncate");
+  Py_RETURN_NONE;
+}
+
+// cache, table_out, refs_out, report, workspace
+PyObject* cache_compact(PyObject* const* a) {
+  const CacheArg c(a[0]);
+  const Arg table(a[1]), refs(a[2]), report(a[3]), ws(a[4]);
+  c.ints(table, c.n_slots() * c.width(), "table_out: contiguous int32, the table's sizes");
+  c.ints(refs, c.n_pages(), "refs_out: contiguous int32, one per page");
+  c.ints(report, 2, "report: contiguous int32 [2]");
+  const Workspace w(ws, c, ws ? 0 : rocs_cache_workspace(c.handle, 0));
+  void* st = stream();
+  check(call([&] {
+          return rocs_cache_compact(c.handle, static_cast<int32_t*>(table.mut()), static_cast<int32_t*>(refs.mut()),
+                                    static_cast<int32_t*>(report.mut()), w.ptr, w.size, st);
+        }),
+        "rocs_cache_compact");
+  Py_RETURN_NONE;
+}
+
+// cache, plan (3), H
+PyObject* cache_attention_workspace(PyObject* const* a) {
+  const CacheArg c(a[0]);
+  const PlanArg plan(a + 1);
+  return PyLong_FromSize_t(rocs_cache_attention_workspace(c.handle, plan.handle, i32(a[4])));
+}
+
+// cache, plan (3), Q, slots, layer, causal, scale, cap, slopes, begin, prefix, out, workspace
+PyObject* cache_attention(PyObject* const* a) {
+  const CacheArg c(a[0]);
+  const PlanArg plan(a + 1);
+  const Arg Q(a[4]), slots(a[5]), slopes(a[10]), begin(a[11]), prefix(a[12]), ws(a[14]);
+  Q.need_dims(3);
+  const int64_t H = Q.size(1);
+  c.rows(Q, plan.N, H, "Q: [N, H, dh] of the cache's type and device, contiguous last dimension");
+  require(H <= 0x7fffffff, "Q: too many heads");
+  Out out(a[13]);
+  out.or_empty({plan.N, H, c.dh()}, Q, Q->scalar_type());
+  c.rows(out.given, plan.N, H, "out: [N, H, dh] of the cache's type and device, contiguous last dimension");
+  const int32_t* sl = c.ints(slots, plan.R, "slots: contiguous int32, one per request");
+  const int32_t* bg = c.ints(begin, plan.N, "begin: contiguous int32, one per row");
+  const int32_t* pf = c.ints(prefix, plan.R, "prefix: contiguous int32, one per request");
+  if (slopes) {
+    c.same(slopes, at::kFloat, "slopes: contiguous float32, one per head");
+    require(slopes->is_contiguous() && slopes->numel() == H, "slopes: contiguous float32, one per head");
+  }
+  const int32_t layer = i32(a[6]);
+  const bool causal = truth(a[7]);
+  const float scale = f32(a[8]), cap = f32(a[9]);
+  const Workspace w(ws, c, ws ? 0 : rocs_cache_attention_workspace(c.handle, plan.handle, (int32_t)H));
+  const int64_t qt = stride_of(Q, 0, H * c.dh()), qh = stride_of(Q, 1, c.dh()), ot = stride_of(out.given, 0, H * c.dh()),
+                oh = stride_of(out.given, 1, c.dh());
+  void* st = stream();
+  check(call([&] {
+          return rocs_cache_attention(c.handle, layer, plan.handle, sl, (int32_t)H, Q.ptr(), qt, qh, causal, scale, cap,
+                                      static_cast<const float*>(slopes.ptr()), bg, pf, out.given.mut(), ot, oh, w.ptr, w.size, st);
+        }),
+        "rocs_cache_attention");
+  return out.release();
+}
+
 PyObject* set_error_type(PyObject* const* a) {
   Py_XSETREF(g_error, Py_NewRef(a[0]));
   Py_RETURN_NONE;
@@ -403,6 +635,16 @@ PyMethodDef methods[] = {ENTRY(plan_create, 2),
                          ENTRY(glm_fm_projection, 9),
                          ENTRY(group_norm, 6),
                          ENTRY(ikbo_linear_static, 8),
+                         ENTRY(cache_create, 5),
+                         ENTRY(cache_destroy, 1),
+                         ENTRY(cache_workspace, 2),
+                         ENTRY(cache_extend, 8),
+                         ENTRY(cache_append, 9),
+                         ENTRY(cache_fork, 5),
+                         ENTRY(cache_truncate, 5),
+                         ENTRY(cache_compact, 5),
+                         ENTRY(cache_attention_workspace, 5),
+                         ENTRY(cache_attention, 15),
                          ENTRY(set_error_type, 1),
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_native", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};

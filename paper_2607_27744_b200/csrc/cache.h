@@ -1,0 +1,24 @@
+// The paged cache of request histories: what a handle names, and what the attention kernels over it are given.
+#pragma once
+#include <cuda.h>
+
+#include "rocs_internal.h"
+
+struct rocs_cache {
+  rocs_dtype_t dtype;
+  int32_t layers, n_pages, page, H_kv, dh;
+  void *K, *V;
+  int64_t ld_layer, ld_page, ld_token, ld_head;  // elements
+  int32_t n_slots, width;
+  int32_t *table, *lens, *refs;
+};
+
+namespace rocs {
+
+int kernel_path();  // of rocs_set_path
+
+#ifdef __CUDACC__
+__device__ __forceinline__ int32_t pages_for(int32_t positions, int32_t page) { return (positions + page - 1) / page; }
+#endif
+
+}  // namespace rocs

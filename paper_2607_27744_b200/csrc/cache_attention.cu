@@ -1,0 +1,495 @@
+// Attention over the paged cache: arguments, choice of kernel, the line of work, the joining of parts, and the general
+// kernel (fp32, head dimensions that the tensor-core kernels do not take).
+#include <algorithm>
+#include <cmath>
+
+#include "cache_attn.cuh"
+
+namespace rocs {
+namespace {
+
+constexpr int kLineThreads = 1024;
+constexpr float kLog2e = 1.4426950408889634f;
+
+// The line of a launch with more tiles than a CTA's shared memory keeps, or whose rows begin somewhere (their first key
+// takes a look at every row: a warp per entry).
+__global__ void __launch_bounds__(kLineThreads, 1) line_kernel(CacheAttn p) {
+  ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  for (int32_t i = warp; i < p.entries; i += kLineThreads / 32) {
+    AttnEntry e = attn_entry(p, i);
+    int32_t first = 0;
+    if (p.begin) {
+      first = 0x7fffffff;
+      for (int32_t t = lane; t < e.count; t += 32) first = min(first, max(p.begin[e.row0 + t], 0));
+      first = __reduce_min_sync(0xffffffffu, first);
+    }
+    attn_blocks(p, e, first);
+    if (lane == 0) p.entries_global[i] = e;
+  }
+  __syncthreads();
+  __shared__ int64_t sums[kLineThreads / 32];
+  int64_t base = 0;
+  for (int32_t i0 = 0; i0 < p.entries; i0 += kLineThreads) {
+    const int32_t i = i0 + (int32_t)threadIdx.x;
+    const int64_t cost = i < p.entries ? attn_cost(p.entries_global[i]) : 0;
+    int64_t incl = cost;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
+    }
+    if (lane == 31) sums[warp] = incl;
+    __syncthreads();
+    int64_t before = base, total = 0;
+    for (int w = 0; w < kLineThreads / 32; ++w) {
+      if (w < warp) before += sums[w];
+      total += sums[w];
+    }
+    if (i < p.entries) p.line_global[i] = before + incl - cost;
+    base += total;
+    __syncthreads();
+  }
+  if (threadIdx.x == 0) p.line_global[p.entries] = base;
+}
+
+template <typename T>
+__device__ __forceinline__ void store_row(uint8_t* out, int32_t c, float v) {
+  if constexpr (sizeof(T) == 4) reinterpret_cast<float*>(out)[c] = v;
+  else reinterpret_cast<__nv_bfloat16*>(out)[c] = __float2bfloat16_rn(v);
+}
+
+// Joins the parts of the tiles that a cut went through: O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i with M the
+// largest reference, part by part in the order of the keys.  A warp per row, its lanes 32 parts' weights first and output
+// columns then; blockIdx.x is the cut.
+constexpr int kJoinThreads = 128;
+template <typename T, int NV>
+__global__ void __launch_bounds__(kJoinThreads) join_kernel(CacheAttn p, int32_t grid) {
+  ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
+  const AttnMeta m = p.meta[blockIdx.x];
+  if (m.end == 0) return;
+  const int64_t total = p.header[0];
+  const int32_t ctas = (int32_t)p.header[1];
+  const AttnEntry e = p.listed ? p.entries_global[m.entry] : attn_entry(p, m.entry);
+  const int lane = threadIdx.x % 32;
+  const int32_t b0 = (int32_t)blockIdx.x - 1;
+  int32_t parts = 1;
+  while (b0 + parts < ctas && AttnWalk::cut(total, ctas, b0 + parts) < m.end) ++parts;
+  const bool first_of_cta = AttnWalk::cut(total, ctas, b0) == m.begin;
+  auto place = [&](int32_t i) { return 2 * (b0 + i) + (i == 0 && !first_of_cta ? 1 : 0); };
+  const int32_t rows = e.count * p.group;
+  for (int32_t row = blockIdx.y * (kJoinThreads / 32) + threadIdx.x / 32; row < rows; row += gridDim.y * (kJoinThreads / 32)) {
+    float M = -INFINITY;
+    for (int32_t i = lane; i < parts; i += 32) M = fmaxf(M, attn_part_sums(p, grid, place(i))[row].x);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
+    float acc[NV], l = 0.f;
+#pragma unroll
+    for (int c = 0; c < NV; ++c) acc[c] = 0.f;
+    for (int32_t i0 = 0; i0 < parts; i0 += 32) {
+      float w = 0.f;
+      if (i0 + lane < parts) {
+        const float2 s = attn_part_sums(p, grid, place(i0 + lane))[row];
+        // a part in which the row saw no key, or only scores of -inf, adds nothing
+        w = s.x == -INFINITY && s.y == 0.f ? 0.f : exp2f((s.x - M) * p.unit);
+        l += s.y == 0.f ? 0.f : w * s.y;
+      }
+      const int32_t here = min(parts - i0, 32);
+#pragma unroll 4
+      for (int32_t k = 0; k < here; ++k) {
+        const float wk = __shfl_sync(0xffffffffu, w, k);
+        if (wk == 0.f) continue;
+        const float* o = attn_part(p, place(i0 + k)) + (int64_t)row * p.dh;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+          if (lane + 32 * c < p.dh) acc[c] = fmaf(wk, o[lane + 32 * c], acc[c]);
+      }
+    }
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+    const int32_t t = row / p.group;
+    const RowKeys keys = attn_row(p, e, t);
+    uint8_t* out = p.O + (int64_t)(e.row0 + t) * p.o_row_bytes + (m.head * p.group + row % p.group) * p.o_head_bytes;
+#pragma unroll
+    for (int c = 0; c < NV; ++c)
+      if (lane + 32 * c < p.dh) store_row<T>(out, lane + 32 * c, keys.lo < keys.hi ? acc[c] / l : 0.f);
+  }
+}
+
+template <typename T>
+rocs_status_t join_parts(const CacheAttn& p, int32_t grid, cudaStream_t stream) {
+  const dim3 blocks((unsigned)grid, (unsigned)std::min(p.tile_rows / 4, 16));
+  if (p.dh <= 64) return launch_dependent(join_kernel<T, 2>, blocks, kJoinThreads, 0, stream, p, grid);
+  if (p.dh <= 128) return launch_dependent(join_kernel<T, 4>, blocks, kJoinThreads, 0, stream, p, grid);
+  return launch_dependent(join_kernel<T, 8>, blocks, kJoinThreads, 0, stream, p, grid);
+}
+
+// ---- general kernel -------------------------------------------------------------------------------
+// 16 rows x blocks of 32 keys on fp32 FMAs, storage fp32 or bf16.  Queries are scaled before the product and scores stay in
+// natural units up to their difference from the reference: whatever scaled score fp32 can hold is a score.  A warp has 4 rows: its lanes are the block's keys for
+// the scores (one key's row of shared memory each, 4 queries broadcast) and output columns for P V (the probabilities
+// broadcast).  K and V blocks are fetched with cp.async, the next while one is used.  Bound by shared-memory reads (5 per
+// 16 FMAs of a score); the rows of a chunk and the keys of a long history are shared over CTAs by the line of work.
+constexpr int kGenThreads = 128, kGenRows = 16, kGenKeys = 32;
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
+  const int n = there ? 16 : 0;  // 0: zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+template <typename T>
+__host__ __device__ constexpr int gen_row_bytes(int dh) { return dh * (int)sizeof(T) + 16; }  // a row's 16-byte vectors fall on other banks than the next one's
+template <typename T>
+constexpr int gen_smem(int dh) { return kGenRows * dh * 4 + 4 * kGenKeys * gen_row_bytes<T>(dh); }
+
+template <typename T, int NV>
+__global__ void __launch_bounds__(kGenThreads) general_kernel(const CacheAttn p) {
+  extern __shared__ __align__(16) uint8_t smem[];
+  __shared__ AttnLine line_mem;
+  __shared__ __align__(16) float probs[kGenThreads / 32][kGenKeys][4];
+  ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
+  const AttnLineView view = attn_line<kGenThreads>(p, line_mem);
+  AttnWalk walk;
+  if (!walk.start(p, view)) return;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
+  const int32_t dh = p.dh, row_bytes = gen_row_bytes<T>(dh), vecs = dh * (int)sizeof(T) / 16;
+  float* qs = reinterpret_cast<float*>(smem);
+  uint8_t* kv = smem + kGenRows * dh * 4;  // [2 stages][K, V][32 keys]
+  const uint32_t kv_addr = ptx::smem_u32(kv);
+  const int32_t block_bytes = kGenKeys * row_bytes;
+
+  for (; walk.more(); walk.next(p, view)) {
+    const AttnEntry e = view.entry[walk.entry];
+    const int32_t kv_head = walk.head / p.per_kv;
+    const int64_t kv_head_bytes = kv_head * p.head_bytes;
+    const int32_t rows = e.count * p.group;
+    __syncthreads();  // the piece in front is done with shared memory
+    for (int32_t x = threadIdx.x; x < kGenRows * dh; x += kGenThreads) {
+      const int32_t row = x / dh, c = x - row * dh;
+      float v = 0.f;
+      if (row < rows) {
+        const uint8_t* q = p.Q + (int64_t)(e.row0 + row / p.group) * p.q_row_bytes + (walk.head * p.group + row % p.group) * p.q_head_bytes;
+        if constexpr (sizeof(T) == 4) v = reinterpret_cast<const float*>(q)[c];
+        else v = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(q)[c]);
+      }
+      qs[x] = v * p.scale;
+    }
+    RowKeys keys[4];
+    float slope[4], m[4], l[4], acc[4][NV];
+    int32_t lo_most = 0, hi_least = 0x7fffffff;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int32_t row = warp * 4 + i;
+      keys[i] = RowKeys{0, 0, 0};
+      slope[i] = 0.f;
+      if (row < rows) {
+        keys[i] = attn_row(p, e, row / p.group);
+        slope[i] = p.slopes ? p.slopes[walk.head * p.group + row % p.group] : 0.f;
+      }
+      lo_most = max(lo_most, keys[i].lo);
+      hi_least = min(hi_least, keys[i].hi);
+      m[i] = -INFINITY;
+      l[i] = 0.f;
+#pragma unroll
+      for (int c = 0; c < NV; ++c) acc[i][c] = 0.f;
+    }
+    const int32_t blk0 = e.blk0 + walk.block0(), blocks = e.blocks > 0 ? walk.blocks() : 0;
+    const int32_t last_key = min(e.L, p.causal ? max(e.pos0 + e.count, e.prefix) : e.L);  // one past the last that any row sees
+    auto load = [&](int32_t b) {
+      const uint32_t dst = kv_addr + (b & 1) * 2 * block_bytes;
+      for (int32_t x = threadIdx.x; x < kGenKeys * vecs; x += kGenThreads) {
+        const int32_t row = x / vecs, v = x - row * vecs, j = (blk0 + b) * kGenKeys + row;
+        const int64_t at = j < last_key ? key_offset(p, e.slot, j) : -1;
+        const int64_t off = at >= 0 ? at + kv_head_bytes + v * 16 : 0;
+        cp_async16(dst + row * row_bytes + v * 16, p.K + off, at >= 0);
+        cp_async16(dst + block_bytes + row * row_bytes + v * 16, p.V + off, at >= 0);
+      }
+      cp_async_commit();
+    };
+    if (blocks > 0) load(0);
+    for (int32_t b = 0; b < blocks; ++b) {
+      if (b + 1 < blocks) {
+        load(b + 1);
+        cp_async_wait<1>();
+      } else {
+        cp_async_wait<0>();
+      }
+      __syncthreads();
+      const uint8_t* kb = kv + (b & 1) * 2 * block_bytes;
+      const uint8_t* vb = kb + block_bytes;
+      const int32_t j0 = (blk0 + b) * kGenKeys, j = j0 + lane;
+      const bool full = j0 >= lo_most && j0 + kGenKeys <= hi_least;
+      float s[4] = {0.f, 0.f, 0.f, 0.f};
+      const float* q = qs + warp * 4 * dh;
+      const uint8_t* kr = kb + lane * row_bytes;
+      for (int32_t v = 0; v < vecs; ++v) {
+        const uint4 raw = *reinterpret_cast<const uint4*>(kr + v * 16);
+        constexpr int kPer = 16 / (int)sizeof(T);
+        float k[kPer];
+        if constexpr (sizeof(T) == 4) {
+          k[0] = __uint_as_float(raw.x); k[1] = __uint_as_float(raw.y); k[2] = __uint_as_float(raw.z); k[3] = __uint_as_float(raw.w);
+        } else {
+          const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+          for (int x = 0; x < 4; ++x) {
+            k[2 * x] = __uint_as_float(w[x] << 16);
+            k[2 * x + 1] = __uint_as_float(w[x] & 0xffff0000u);
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+#pragma unroll
+          for (int x = 0; x < kPer; x += 4) {
+            const float4 qv = *reinterpret_cast<const float4*>(q + i * dh + v * kPer + x);
+            s[i] = fmaf(qv.x, k[x], s[i]);
+            s[i] = fmaf(qv.y, k[x + 1], s[i]);
+            s[i] = fmaf(qv.z, k[x + 2], s[i]);
+            s[i] = fmaf(qv.w, k[x + 3], s[i]);
+          }
+      }
+      float pr[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float x = s[i];
+        if (p.cap > 0.f) x = p.cap * tanhf(x);
+        if (p.slopes) x -= slope[i] * fabsf((float)(keys[i].pos - j));
+        if (!full && (j < keys[i].lo || j >= keys[i].hi)) x = -INFINITY;
+        float mx = x;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const float m_new = fmaxf(m[i], mx);
+        const float a = m[i] == m_new ? 1.f : exp2f((m[i] - m_new) * kLog2e);  // (both -inf: nothing yet)
+        pr[i] = x == -INFINITY ? 0.f : exp2f((x - m_new) * kLog2e);
+        l[i] = fmaf(l[i], a, pr[i]);
+        m[i] = m_new;
+        if (a != 1.f)
+#pragma unroll
+          for (int c = 0; c < NV; ++c) acc[i][c] *= a;
+      }
+      *reinterpret_cast<float4*>(probs[warp][lane]) = make_float4(pr[0], pr[1], pr[2], pr[3]);
+      __syncwarp();
+      auto add_values = [&](bool masked) {
+#pragma unroll 4
+        for (int k = 0; k < kGenKeys; ++k) {
+          const float4 w = *reinterpret_cast<const float4*>(probs[warp][k]);
+          const uint8_t* vr = vb + k * row_bytes;
+#pragma unroll
+          for (int c = 0; c < NV; ++c) {
+            const int32_t d = lane + 32 * c;
+            if (d >= dh) continue;
+            float x;
+            if constexpr (sizeof(T) == 4) x = reinterpret_cast<const float*>(vr)[d];
+            else x = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(vr)[d]);
+            // a key that a row does not see adds nothing, whatever its value holds
+            if (!masked || w.x != 0.f) acc[0][c] = fmaf(w.x, x, acc[0][c]);
+            if (!masked || w.y != 0.f) acc[1][c] = fmaf(w.y, x, acc[1][c]);
+            if (!masked || w.z != 0.f) acc[2][c] = fmaf(w.z, x, acc[2][c]);
+            if (!masked || w.w != 0.f) acc[3][c] = fmaf(w.w, x, acc[3][c]);
+          }
+        }
+      };
+      if (full) add_values(false); else add_values(true);
+      __syncthreads();  // the block's place may be loaded into
+    }
+    const bool whole = walk.whole();
+    const int32_t part = walk.part();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int32_t row = warp * 4 + i;
+#pragma unroll
+      for (int o = 16; o > 0; o >>= 1) l[i] += __shfl_xor_sync(0xffffffffu, l[i], o);
+      if (row >= rows) continue;
+      if (whole) {
+        uint8_t* out = p.O + (int64_t)(e.row0 + row / p.group) * p.o_row_bytes + (walk.head * p.group + row % p.group) * p.o_head_bytes;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+          if (lane + 32 * c < dh) store_row<T>(out, lane + 32 * c, keys[i].lo < keys[i].hi ? acc[i][c] / l[i] : 0.f);
+      } else {
+        float* o = attn_part(p, part) + (int64_t)row * dh;
+#pragma unroll
+        for (int c = 0; c < NV; ++c)
+          if (lane + 32 * c < dh) o[lane + 32 * c] = acc[i][c];
+        if (lane == 0) attn_part_sums(p, gridDim.x, part)[row] = make_float2(m[i], l[i]);
+      }
+    }
+  }
+}
+
+template <typename T, int NV>
+rocs_status_t launch_general(const CacheAttn& p, int32_t grid, cudaStream_t stream) {
+  auto kernel = general_kernel<T, NV>;
+  ROCS_ALLOW_SMEM(kernel, gen_smem<T>(32 * NV));
+  return launch_dependent(kernel, dim3((unsigned)grid), kGenThreads, (size_t)gen_smem<T>(p.dh), stream, p);
+}
+template <typename T>
+rocs_status_t general_of(const CacheAttn& p, int32_t grid, cudaStream_t stream) {
+  if (p.dh <= 32) return launch_general<T, 1>(p, grid, stream);
+  if (p.dh <= 64) return launch_general<T, 2>(p, grid, stream);
+  if (p.dh <= 128) return launch_general<T, 4>(p, grid, stream);
+  return launch_general<T, 8>(p, grid, stream);
+}
+
+int sm_count() {
+  int dev = 0, n = 148;
+  if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
+  return n;
+}
+
+enum class Kind { kGeneral };
+
+// Which kernel a call takes, and how its work is cut.
+struct Choice {
+  Kind kind;
+  int32_t group, per_kv, heads;  // query heads per tile row, such groups per key head, groups in all
+  int32_t rows_per_tile, tile_rows, block, min_units, grid;
+  int64_t entries;
+  bool by_request;  // no request has more than one tile
+};
+Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H) {
+  Choice x{};
+  const int32_t g = H / c->H_kv, sms = sm_count();
+  int32_t most = 16;
+  x.kind = Kind::kGeneral;
+  x.block = kGenKeys;
+  // the CTAs of one round of the chip: 128 registers a thread, and shared memory (with the line and the probabilities)
+  const int smem = (c->dtype == ROCS_BF16 ? gen_smem<__nv_bfloat16>(c->dh) : gen_smem<float>(c->dh)) + (int)sizeof(AttnLine) + 4096;
+  x.grid = sms * std::min(4, 228 * 1024 / smem);
+  x.min_units = 2;
+  x.group = 1;  // the largest part of the heads of a key head that fits a tile
+  for (int32_t d = std::min(g, most); d >= 1; --d)
+    if (g % d == 0) { x.group = d; break; }
+  x.per_kv = g / x.group;
+  x.heads = H / x.group;
+  x.rows_per_tile = most / x.group;
+  x.tile_rows = most;
+  x.by_request = plan->largest <= x.rows_per_tile;
+  x.entries = x.by_request ? plan->R : plan_entries(plan, x.rows_per_tile);
+  return x;
+}
+
+struct Places {
+  size_t meta, line, entries, parts, bytes;
+};
+Places places(const Choice& x, int32_t dh) {
+  Places w;
+  w.meta = 256;
+  w.line = w.meta + round_up(sizeof(AttnMeta) * (size_t)x.grid, 256);
+  w.entries = w.line + round_up(sizeof(int64_t) * ((size_t)x.entries + 1), 256);
+  w.parts = w.entries + round_up(sizeof(AttnEntry) * (size_t)x.entries, 256);
+  w.bytes = w.parts + round_up(2 * (size_t)x.grid * x.tile_rows * ((size_t)dh + 2) * sizeof(float), 256);
+  return w;
+}
+
+bool strides_ok(int64_t ld_row, int64_t ld_head, int64_t es) {
+  return ld_row >= 0 && ld_head >= 0 && ld_row * es % 16 == 0 && ld_head * es % 16 == 0;
+}
+
+}  // namespace
+
+rocs_status_t attn_general(rocs_dtype_t dt, const CacheAttn& p, int32_t grid, cudaStream_t stream) {
+  return dt == ROCS_BF16 ? general_of<__nv_bfloat16>(p, grid, stream) : general_of<float>(p, grid, stream);
+}
+
+}  // namespace rocs
+
+using namespace rocs;
+
+extern "C" {
+
+size_t rocs_cache_attention_workspace(const rocs_cache_t* c, const rocs_plan_t* plan, int32_t H) {
+  if (!c || !plan || H < 1 || H % c->H_kv != 0) return 0;
+  return places(choose(c, plan, H), c->dh).bytes;
+}
+
+rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const rocs_plan_t* plan, const int32_t* slots, int32_t H,
+                                   const void* Q, int64_t ld_qt, int64_t ld_qh, int32_t causal, float scale, float cap,
+                                   const float* slopes, const int32_t* begin, const int32_t* prefix, void* O, int64_t ld_ot,
+                                   int64_t ld_oh, void* workspace, size_t bytes, void* stream_) {
+  if (!c || !plan || layer < 0 || layer >= c->layers || H < 1 || H % c->H_kv != 0) return ROCS_ERR_INVALID_ARG;
+  if ((!causal && prefix) || !(cap >= 0.f) || std::isinf(cap) || !std::isfinite(scale)) return ROCS_ERR_INVALID_ARG;
+  if (plan->N == 0) return ROCS_OK;
+  if (!Q || !O) return ROCS_ERR_INVALID_ARG;
+  const int64_t es = (int64_t)elem_size(c->dtype);
+  if (!aligned16(Q) || !aligned16(O) || !strides_ok(ld_qt, ld_qh, es) || !strides_ok(ld_ot, ld_oh, es)) return ROCS_ERR_ALIGNMENT;
+  if ((H > 1 && ld_oh < c->dh) || (plan->N > 1 && ld_ot < c->dh)) return ROCS_ERR_INVALID_ARG;  // rows of O share no memory
+  if (H > 65535) return ROCS_ERR_UNSUPPORTED;
+  if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)c->dh);
+  const Choice x = choose(c, plan, H);
+  const Places w = places(x, c->dh);
+  if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || bytes < w.bytes) return ROCS_ERR_WORKSPACE;
+  if (x.entries > 0x7fffffffLL) return ROCS_ERR_UNSUPPORTED;
+  cudaStream_t stream = (cudaStream_t)stream_;
+  CacheAttn p{};
+  p.K = static_cast<const uint8_t*>(c->K) + layer * c->ld_layer * es;
+  p.V = static_cast<const uint8_t*>(c->V) + layer * c->ld_layer * es;
+  p.page_bytes = c->ld_page * es;
+  p.token_bytes = c->ld_token * es;
+  p.head_bytes = c->ld_head * es;
+  p.n_pages = c->n_pages;
+  p.page = c->page;
+  p.page_shift = -1;
+  for (int s = 0; s < 31; ++s)
+    if (c->page == (1 << s)) p.page_shift = s;
+  p.dh = c->dh;
+  p.n_slots = c->n_slots;
+  p.width = c->width;
+  p.table = c->table;
+  p.lens = c->lens;
+  p.slots = slots;
+  p.off = plan->cand_offsets;
+  p.begin = begin;
+  p.prefix = prefix;
+  p.entries = (int32_t)x.entries;
+  p.causal = causal != 0;
+  p.group = x.group;
+  p.heads = x.heads;
+  p.per_kv = x.per_kv;
+  p.rows_per_tile = x.rows_per_tile;
+  p.R = plan->R;
+  p.Q = static_cast<const uint8_t*>(Q);
+  p.O = static_cast<uint8_t*>(O);
+  p.q_row_bytes = ld_qt * es;
+  p.q_head_bytes = ld_qh * es;
+  p.o_row_bytes = ld_ot * es;
+  p.o_head_bytes = ld_oh * es;
+  p.unit = x.kind == Kind::kGeneral ? kLog2e : 1.f;
+  const float to_unit = x.kind == Kind::kGeneral ? 1.f : kLog2e;
+  p.scale = cap > 0.f ? scale / cap : scale * to_unit;
+  p.cap = cap * to_unit;
+  p.slopes = slopes;
+  p.block = x.block;
+  p.min_units = x.min_units;
+  p.tile_rows = x.tile_rows;
+  uint8_t* ws = static_cast<uint8_t*>(workspace);
+  p.header = reinterpret_cast<int64_t*>(ws);
+  p.meta = reinterpret_cast<AttnMeta*>(ws + w.meta);
+  p.line_global = reinterpret_cast<int64_t*>(ws + w.line);
+  p.entries_global = reinterpret_cast<AttnEntry*>(ws + w.entries);
+  p.parts = reinterpret_cast<float*>(ws + w.parts);
+  p.status = device_status_word();
+  if (!p.status) return ROCS_ERR_CUDA;
+  if (!x.by_request) {
+    TileList tiles;
+    const rocs_status_t st = plan_tiles(plan, x.rows_per_tile, stream, &tiles);
+    if (st != ROCS_OK) return st;
+    p.tiles = tiles.dev;
+  }
+  p.listed = x.entries > kLocalEntries || (begin && x.rows_per_tile > 8);
+  if (p.listed) {
+    const rocs_status_t st = launch_dependent(line_kernel, dim3(1), kLineThreads, 0, stream, p);
+    if (st != ROCS_OK) return st;
+  }
+  const rocs_status_t st = attn_general(c->dtype, p, x.grid, stream);
+  if (st != ROCS_OK) return st;
+  return c->dtype == ROCS_BF16 ? join_parts<__nv_bfloat16>(p, x.grid, stream) : join_parts<float>(p, x.grid, stream);
+}
+
+}  // extern "C"

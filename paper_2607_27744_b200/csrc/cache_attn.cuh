@@ -1,0 +1,235 @@
+// What the attention kernels over the paged cache share: parameters, the rows' visible keys, and the division of a
+// launch's work.
+//
+// Work is counted in key blocks.  A tile is a run of a request's rows under one key head; it costs as many units as it has
+// key blocks (one if it has none: zeros are written).  All tiles of the launch stand in a line, tile by tile and inside
+// one block by block, and the line is cut into as many equal pieces as there are CTAs: every CTA gets the same number of
+// blocks whatever the lengths, which only the device knows.  A tile that a cut goes through leaves unnormalised parts in
+// the workspace, and a second small kernel joins them in the order of the keys.  At most two parts per CTA.
+#pragma once
+#include <cuda_bf16.h>
+
+#include "cache.h"
+#include "sm100_ptx.cuh"
+
+namespace rocs {
+
+constexpr int kLocalEntries = 256;  // up to this many tiles (without heads) every CTA finds the line itself
+
+// A run of rows of one request: everything a kernel has to know about it but the head.
+struct AttnEntry {
+  int32_t slot;     // -1: none
+  int32_t L;        // keys of the slot
+  int32_t row0, count;  // rows of the batch
+  int32_t pos0;     // where the first of them stands
+  int32_t prefix;   // keys visible to all rows
+  int32_t blk0, blocks;
+};
+
+struct AttnMeta {   // of a CTA whose first piece continues a tile that the CTA in front began
+  int64_t begin, end;  // units of the tile; end 0: no such piece
+  int32_t entry, head;
+  int64_t pad;
+};
+
+struct CacheAttn {
+  const uint8_t *K, *V;  // of the layer
+  int64_t page_bytes, token_bytes, head_bytes;
+  int32_t n_pages, page, page_shift;  // page_shift < 0: not a power of two
+  int32_t dh, n_slots, width;
+  const int32_t *table, *lens, *slots, *off, *begin, *prefix;
+  const Tile* tiles;  // null: request e is entry e
+  int32_t entries, causal;
+  // query heads: `group` of them per tile row, `heads` groups, `per_kv` groups per key head
+  int32_t group, heads, per_kv, rows_per_tile;  // rows_per_tile: of the batch
+  int32_t R;
+  const uint8_t* Q;
+  uint8_t* O;
+  int64_t q_row_bytes, q_head_bytes, o_row_bytes, o_head_bytes;
+  // scores in units of 1 / unit powers of two: scale * log2(e) / unit; capped: scale / cap, then cap * log2(e) / unit
+  float scale, cap, unit;
+  const float* slopes;
+  int32_t block, min_units; // keys per unit, least units of a CTA
+  int32_t tile_rows;        // rows of a tile as the parts hold them (batch rows x group, rounded up)
+  // workspace
+  int64_t* line_global;     // [entries + 1]
+  AttnEntry* entries_global;
+  bool listed;              // the two above were made by a launch in front
+  int64_t* header;          // [0] units of the line, [1] CTAs that share it
+  AttnMeta* meta;           // [CTAs]
+  float* parts;             // [2 CTAs][tile_rows][dh], then [2 CTAs][tile_rows][2]: reference and sum
+  uint32_t* status;
+};
+
+#ifdef __CUDACC__
+struct AttnLine {
+  int64_t line[kLocalEntries + 1];
+  AttnEntry entry[kLocalEntries];
+};
+struct AttnLineView {
+  const int64_t* line;
+  const AttnEntry* entry;
+};
+
+// The first keys and one past the last that batch row `row0 + t` of the entry sees, and where the row stands.
+struct RowKeys {
+  int32_t lo, hi, pos;
+};
+__device__ __forceinline__ RowKeys attn_row(const CacheAttn& p, const AttnEntry& e, int32_t t) {
+  RowKeys k;
+  k.pos = p.causal ? e.pos0 + t : e.pos0;
+  k.lo = p.begin ? max(p.begin[e.row0 + t], 0) : 0;
+  k.hi = p.causal ? min(max(k.pos + 1, e.prefix), e.L) : e.L;
+  return k;
+}
+
+// Entry i but for its first visible key, which takes all of its rows where rows begin somewhere.
+__device__ __forceinline__ AttnEntry attn_entry(const CacheAttn& p, int32_t i) {
+  AttnEntry e;
+  int32_t r = i, n;
+  if (p.tiles != nullptr) {
+    const Tile t = p.tiles[i];
+    r = t.req;
+    e.row0 = t.cand0;
+    e.count = t.count;
+    n = p.off[r + 1] - p.off[r];
+  } else {
+    e.row0 = p.off[r];
+    e.count = n = p.off[r + 1] - e.row0;
+  }
+  const int32_t s = p.slots ? p.slots[r] : r;
+  e.slot = s >= 0 && s < p.n_slots ? s : -1;
+  e.L = e.slot >= 0 ? min(max(p.lens[e.slot], 0), p.width * p.page) : 0;
+  e.pos0 = p.causal ? e.L - n + (e.row0 - p.off[r]) : e.L;
+  e.prefix = p.causal && p.prefix ? max(p.prefix[r], 0) : 0;
+  return e;
+}
+__device__ __forceinline__ void attn_blocks(const CacheAttn& p, AttnEntry& e, int32_t first_key) {
+  const int32_t last = p.causal ? min(max(e.pos0 + e.count, e.prefix), e.L) : e.L;
+  e.blk0 = first_key / p.block;
+  e.blocks = last > first_key ? (last + p.block - 1) / p.block - e.blk0 : 0;
+}
+__device__ __forceinline__ int64_t attn_cost(const AttnEntry& e) { return e.count > 0 ? max(e.blocks, 1) : 0; }
+
+// The line, found by the CTA's THREADS threads (all call this) or by the launch in front.
+template <int THREADS>
+__device__ __forceinline__ AttnLineView attn_line(const CacheAttn& p, AttnLine& mem) {
+  if (p.listed) return AttnLineView{p.line_global, p.entries_global};
+  for (int32_t i = threadIdx.x; i < p.entries; i += THREADS) {
+    AttnEntry e = attn_entry(p, i);
+    int32_t first = 0;
+    if (p.begin) {
+      first = 0x7fffffff;
+      for (int32_t t = 0; t < e.count; ++t) first = min(first, max(p.begin[e.row0 + t], 0));
+    }
+    attn_blocks(p, e, first);
+    mem.entry[i] = e;
+  }
+  __syncthreads();
+  if (threadIdx.x < 32) {
+    int64_t base = 0;
+    for (int32_t i0 = 0; i0 < p.entries; i0 += 32) {
+      const int32_t i = i0 + (int32_t)threadIdx.x;
+      const int64_t cost = i < p.entries ? attn_cost(mem.entry[i]) : 0;
+      int64_t incl = cost;
+#pragma unroll
+      for (int o = 1; o < 32; o <<= 1) {
+        const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
+        if ((int)threadIdx.x >= o) incl += up;
+      }
+      if (i < p.entries) mem.line[i] = base + incl - cost;
+      base += __shfl_sync(0xffffffffu, incl, 31);
+    }
+    if (threadIdx.x == 0) mem.line[p.entries] = base;
+  }
+  __syncthreads();
+  return AttnLineView{mem.line, mem.entry};
+}
+
+// A CTA's way along its piece of the line.
+struct AttnWalk {
+  int64_t u, end;      // units
+  int64_t tile_begin;  // unit at which the tile at hand begins
+  int32_t entry, head, cost;
+  bool first;          // the piece at hand is the CTA's first
+  __device__ __forceinline__ static int64_t cut(int64_t total, int32_t ctas, int32_t i) { return total * i / ctas; }
+  // false: nothing for this CTA.  CTA 0 notes what the joining kernel needs.
+  __device__ __forceinline__ bool start(const CacheAttn& p, const AttnLineView& v) {
+    const int64_t total = v.line[p.entries] * p.heads;
+    const int32_t ctas = (int32_t)min((int64_t)gridDim.x, max(total / p.min_units, (int64_t)1));
+    const int32_t i = blockIdx.x;
+    if (i == 0 && threadIdx.x == 0) {
+      p.header[0] = total;
+      p.header[1] = ctas;
+    }
+    u = end = 0;
+    first = true;
+    if (i >= ctas || total == 0) {
+      if (threadIdx.x == 0) p.meta[i].end = 0;
+      return false;
+    }
+    u = cut(total, ctas, i);
+    end = cut(total, ctas, i + 1);
+    int32_t lo = 0, hi = p.entries;  // largest entry that begins at or before u
+    while (hi - lo > 1) {
+      const int32_t mid = lo + (hi - lo) / 2;
+      if (v.line[mid] * p.heads <= u) lo = mid; else hi = mid;
+    }
+    entry = lo;
+    cost = (int32_t)(v.line[lo + 1] - v.line[lo]);
+    const int64_t in = u - v.line[lo] * p.heads;
+    head = (int32_t)(in / cost);
+    tile_begin = v.line[lo] * p.heads + (int64_t)head * cost;
+    if (threadIdx.x == 0) {
+      const bool joins = u > tile_begin && cut(total, ctas, i - 1) <= tile_begin;
+      AttnMeta m;
+      m.begin = tile_begin;
+      m.end = joins ? tile_begin + cost : 0;
+      m.entry = entry;
+      m.head = head;
+      p.meta[i] = m;
+    }
+    return true;
+  }
+  __device__ __forceinline__ bool more() const { return u < end; }
+  __device__ __forceinline__ int32_t block0() const { return (int32_t)(u - tile_begin); }
+  __device__ __forceinline__ int32_t blocks() const { return (int32_t)(min(end, tile_begin + cost) - u); }
+  __device__ __forceinline__ bool whole() const { return u == tile_begin && end >= tile_begin + cost; }
+  // where a part goes: a CTA's first piece to its first place, otherwise (its last) to the second
+  __device__ __forceinline__ int32_t part() const { return 2 * (int32_t)blockIdx.x + (first ? 0 : 1); }
+  __device__ __forceinline__ void next(const CacheAttn& p, const AttnLineView& v) {
+    u += blocks();
+    first = false;
+    if (u >= end) return;
+    tile_begin += cost;
+    if (++head == p.heads) {
+      head = 0;
+      do ++entry; while (v.line[entry + 1] == v.line[entry]);
+      cost = (int32_t)(v.line[entry + 1] - v.line[entry]);
+    }
+  }
+};
+
+__device__ __forceinline__ float* attn_part(const CacheAttn& p, int32_t part) { return p.parts + (int64_t)part * p.tile_rows * p.dh; }
+__device__ __forceinline__ float2* attn_part_sums(const CacheAttn& p, int32_t ctas_of_grid, int32_t part) {
+  return reinterpret_cast<float2*>(p.parts + 2 * (int64_t)ctas_of_grid * p.tile_rows * p.dh) + (int64_t)part * p.tile_rows;
+}
+
+__device__ __forceinline__ int32_t page_of(const CacheAttn& p, int32_t j) { return p.page_shift >= 0 ? j >> p.page_shift : j / p.page; }
+
+// Byte offset of key j of the slot in K or V (without the head), -1 where its page is none of the pool's.
+__device__ __forceinline__ int64_t key_offset(const CacheAttn& p, int32_t slot, int32_t j) {
+  const int32_t at = page_of(p, j), id = p.table[(int64_t)slot * p.width + at];
+  if (id < 0 || id >= p.n_pages) return -1;
+  return id * p.page_bytes + (int64_t)(j - at * p.page) * p.token_bytes;
+}
+
+__device__ __forceinline__ float slope_of(const CacheAttn& p, int32_t q_head) {
+  return p.slopes ? p.slopes[q_head] * 1.4426950408889634f : 0.f;
+}
+#endif
+
+// The kernels.  Each takes the launch's parameters; the grid is the number of CTAs that may share the line.
+rocs_status_t attn_general(rocs_dtype_t dt, const CacheAttn& p, int32_t grid, cudaStream_t stream);
+
+}  // namespace rocs

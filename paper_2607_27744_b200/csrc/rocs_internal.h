@@ -53,6 +53,7 @@ struct DcaItemList {
 struct rocs_plan {
   int32_t R = 0;
   int64_t N = 0;
+  int32_t largest = 0;                    // candidates of the request with the most
   const int32_t* cand_offsets = nullptr;  // device, borrowed
   std::vector<int32_t> offsets_host;      // [R+1]
   mutable std::mutex mu;
