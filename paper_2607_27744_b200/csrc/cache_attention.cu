@@ -134,16 +134,6 @@ rocs_status_t join_parts(const CacheAttn& p, int32_t grid, cudaStream_t stream) 
 // 16 FMAs of a score); the rows of a chunk and the keys of a long history are shared over CTAs by the line of work.
 constexpr int kGenThreads = 128, kGenRows = 16, kGenKeys = 32;
 
-__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
-  const int n = there ? 16 : 0;  // 0: zeros
-  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
-}
-__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void cp_async_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
 template <typename T>
 __host__ __device__ constexpr int gen_row_bytes(int dh) { return dh * (int)sizeof(T) + 16; }  // a row's 16-byte vectors fall on other banks than the next one's
 template <typename T>
@@ -343,7 +333,7 @@ int sm_count() {
   return n;
 }
 
-enum class Kind { kGeneral };
+enum class Kind { kGeneral, kMma };
 
 // Which kernel a call takes, and how its work is cut.
 struct Choice {
@@ -359,10 +349,15 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H) {
   int32_t most = 16;
   x.kind = Kind::kGeneral;
   x.block = kGenKeys;
+  x.min_units = 2;
+  if (c->dtype == ROCS_BF16 && kernel_path() == ROCS_PATH_AUTO && (c->dh == 32 || c->dh == 64 || c->dh == 128)) {
+    x.kind = Kind::kMma;
+    x.block = kMmaKeys;
+    if ((int64_t)plan->largest * g > 16) most = 64;
+  }
   // the CTAs of one round of the chip: 128 registers a thread, and shared memory (with the line and the probabilities)
   const int smem = (c->dtype == ROCS_BF16 ? gen_smem<__nv_bfloat16>(c->dh) : gen_smem<float>(c->dh)) + (int)sizeof(AttnLine) + 4096;
-  x.grid = sms * std::min(4, 228 * 1024 / smem);
-  x.min_units = 2;
+  x.grid = sms * (x.kind == Kind::kMma ? attn_mma_ctas_per_sm(c->dh) : std::min(4, 228 * 1024 / smem));
   x.group = 1;  // the largest part of the heads of a key head that fits a tile
   for (int32_t d = std::min(g, most); d >= 1; --d)
     if (g % d == 0) { x.group = d; break; }
@@ -487,7 +482,7 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
     const rocs_status_t st = launch_dependent(line_kernel, dim3(1), kLineThreads, 0, stream, p);
     if (st != ROCS_OK) return st;
   }
-  const rocs_status_t st = attn_general(c->dtype, p, x.grid, stream);
+  const rocs_status_t st = x.kind == Kind::kMma ? attn_mma(p, x.grid, stream) : attn_general(c->dtype, p, x.grid, stream);
   if (st != ROCS_OK) return st;
   return c->dtype == ROCS_BF16 ? join_parts<__nv_bfloat16>(p, x.grid, stream) : join_parts<float>(p, x.grid, stream);
 }

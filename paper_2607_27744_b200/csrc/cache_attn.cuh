@@ -14,7 +14,7 @@
 
 namespace rocs {
 
-constexpr int kLocalEntries = 256;  // up to this many tiles (without heads) every CTA finds the line itself
+constexpr int kLocalEntries = 128;  // up to this many tiles (without heads) every CTA finds the line itself
 
 // A run of rows of one request: everything a kernel has to know about it but the head.
 struct AttnEntry {
@@ -224,6 +224,96 @@ __device__ __forceinline__ int64_t key_offset(const CacheAttn& p, int32_t slot, 
   return id * p.page_bytes + (int64_t)(j - at * p.page) * p.token_bytes;
 }
 
+__device__ __forceinline__ float ex2_approx(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// tanh(t) = 1 - 2 / (1 + e^2t), absolute error about 1e-7 (two instructions of the special-function unit; tanh.approx is
+// one, and 2^-11 off, which capped scores of 50 would show).
+__device__ __forceinline__ float tanh_fast(float t) {
+  float r;
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2_approx(t * 2.8853900817779268f)));
+  return fmaf(-2.f, r, 1.f);
+}
+
+__device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
+  const int n = there ? 16 : 0;  // 0: zeros
+  asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(n) : "memory");
+}
+__device__ __forceinline__ void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N>
+__device__ __forceinline__ void cp_async_wait() {
+  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
+}
+
+__device__ __forceinline__ uint32_t bf16_pair(float lo, float hi) {
+  const __nv_bfloat162 h2 = __floats2bfloat162_rn(lo, hi);
+  return *reinterpret_cast<const uint32_t*>(&h2);
+}
+
+// One row over keys k0..k1-1, by one warp in fp32: reference m (log2 units), sum l, unnormalised output columns
+// lane + 32 c.  For rows of the tensor-core kernels that came out non-finite: there a key that the row does not see has
+// weight 0, but 0 x (NaN or Inf in its value) is not 0.  Here such keys are not looked at; what is not finite because of
+// keys that the row does see comes out the same again.
+template <int DH>
+__device__ __forceinline__ void attn_row_by_hand(const CacheAttn& p, const AttnEntry& e, int64_t kv_head_bytes, const uint8_t* q_row,
+                                                 const RowKeys& keys, float slope, int32_t k0, int32_t k1, float& m, float& l,
+                                                 float (&acc)[DH / 32]) {
+  const int lane = threadIdx.x % 32;
+  m = -INFINITY;
+  l = 0.f;
+#pragma unroll
+  for (int c = 0; c < DH / 32; ++c) acc[c] = 0.f;
+  k0 = max(k0, keys.lo);
+  k1 = min(k1, keys.hi);
+  for (int32_t j0 = k0; j0 < k1; j0 += 32) {
+    const int32_t j = j0 + lane;
+    float x = -INFINITY;
+    const int64_t off = j < k1 ? key_offset(p, e.slot, j) : -1;
+    if (j < k1) {
+      float s = 0.f;
+      if (off >= 0) {
+        const uint4* k = reinterpret_cast<const uint4*>(p.K + off + kv_head_bytes);
+        const uint4* q = reinterpret_cast<const uint4*>(q_row);
+#pragma unroll 1
+        for (int v = 0; v < DH / 8; ++v) {
+          const uint4 a = k[v], b = q[v];
+          const uint32_t ka[4] = {a.x, a.y, a.z, a.w}, qb[4] = {b.x, b.y, b.z, b.w};
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            s = fmaf(__uint_as_float(qb[i] << 16), __uint_as_float(ka[i] << 16), s);
+            s = fmaf(__uint_as_float(qb[i] & 0xffff0000u), __uint_as_float(ka[i] & 0xffff0000u), s);
+          }
+        }
+      }
+      x = s * p.scale;
+      if (p.cap > 0.f) x = p.cap * tanh_fast(x);
+      if (p.slopes) x -= slope * fabsf((float)(keys.pos - j));
+    }
+    float mx = x;
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    const float m_new = fmaxf(m, mx), a = m == m_new ? 1.f : exp2f(m - m_new);
+    const float w = x == -INFINITY ? 0.f : exp2f(x - m_new);
+    l = fmaf(l, a, w);
+    m = m_new;
+#pragma unroll
+    for (int c = 0; c < DH / 32; ++c) acc[c] *= a;
+    const int32_t here = min(32, k1 - j0);
+    for (int32_t k = 0; k < here; ++k) {
+      const float wk = __shfl_sync(0xffffffffu, w, k);
+      const int64_t at = __shfl_sync(0xffffffffu, off, k);
+      if (at < 0) continue;
+      const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(p.V + at + kv_head_bytes);
+#pragma unroll
+      for (int c = 0; c < DH / 32; ++c) acc[c] = fmaf(wk, __bfloat162float(v[lane + 32 * c]), acc[c]);
+    }
+  }
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
+}
+
 __device__ __forceinline__ float slope_of(const CacheAttn& p, int32_t q_head) {
   return p.slopes ? p.slopes[q_head] * 1.4426950408889634f : 0.f;
 }
@@ -231,5 +321,9 @@ __device__ __forceinline__ float slope_of(const CacheAttn& p, int32_t q_head) {
 
 // The kernels.  Each takes the launch's parameters; the grid is the number of CTAs that may share the line.
 rocs_status_t attn_general(rocs_dtype_t dt, const CacheAttn& p, int32_t grid, cudaStream_t stream);
+// bf16, head dimension 32, 64 or 128, on warp-level tensor cores; tiles of 16 rows (keys split over the warps) or 64.
+constexpr int kMmaKeys = 64;
+int attn_mma_ctas_per_sm(int32_t dh);
+rocs_status_t attn_mma(const CacheAttn& p, int32_t grid, cudaStream_t stream);
 
 }  // namespace rocs
