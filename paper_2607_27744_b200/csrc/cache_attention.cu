@@ -333,7 +333,7 @@ int sm_count() {
   return n;
 }
 
-enum class Kind { kGeneral, kMma };
+enum class Kind { kGeneral, kMma, kUmma };
 
 // Which kernel a call takes, and how its work is cut.
 struct Choice {
@@ -354,17 +354,23 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H) {
     x.kind = Kind::kMma;
     x.block = kMmaKeys;
     if ((int64_t)plan->largest * g > 16) most = 64;
+    if ((int64_t)plan->largest * g > 64 && attn_umma_supported(c->dh, c->page)) {
+      x.kind = Kind::kUmma;
+      x.block = kUmmaKeys;
+      most = 128;  // of a side
+    }
   }
   // the CTAs of one round of the chip: 128 registers a thread, and shared memory (with the line and the probabilities)
   const int smem = (c->dtype == ROCS_BF16 ? gen_smem<__nv_bfloat16>(c->dh) : gen_smem<float>(c->dh)) + (int)sizeof(AttnLine) + 4096;
-  x.grid = sms * (x.kind == Kind::kMma ? attn_mma_ctas_per_sm(c->dh) : std::min(4, 228 * 1024 / smem));
+  x.grid = sms * (x.kind == Kind::kUmma ? 1 : x.kind == Kind::kMma ? attn_mma_ctas_per_sm(c->dh) : std::min(4, 228 * 1024 / smem));
   x.group = 1;  // the largest part of the heads of a key head that fits a tile
   for (int32_t d = std::min(g, most); d >= 1; --d)
     if (g % d == 0) { x.group = d; break; }
   x.per_kv = g / x.group;
   x.heads = H / x.group;
-  x.rows_per_tile = most / x.group;
-  x.tile_rows = most;
+  const int32_t sides = x.kind == Kind::kUmma ? 2 : 1;
+  x.rows_per_tile = sides * (most / x.group);
+  x.tile_rows = sides * most;
   x.by_request = plan->largest <= x.rows_per_tile;
   x.entries = x.by_request ? plan->R : plan_entries(plan, x.rows_per_tile);
   return x;
@@ -482,7 +488,9 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
     const rocs_status_t st = launch_dependent(line_kernel, dim3(1), kLineThreads, 0, stream, p);
     if (st != ROCS_OK) return st;
   }
-  const rocs_status_t st = x.kind == Kind::kMma ? attn_mma(p, x.grid, stream) : attn_general(c->dtype, p, x.grid, stream);
+  const rocs_status_t st = x.kind == Kind::kUmma  ? attn_umma(p, H, c->H_kv, plan->N, x.grid, stream)
+                           : x.kind == Kind::kMma ? attn_mma(p, x.grid, stream)
+                                                  : attn_general(c->dtype, p, x.grid, stream);
   if (st != ROCS_OK) return st;
   return c->dtype == ROCS_BF16 ? join_parts<__nv_bfloat16>(p, x.grid, stream) : join_parts<float>(p, x.grid, stream);
 }

@@ -325,5 +325,9 @@ rocs_status_t attn_general(rocs_dtype_t dt, const CacheAttn& p, int32_t grid, cu
 constexpr int kMmaKeys = 64;
 int attn_mma_ctas_per_sm(int32_t dh);
 rocs_status_t attn_mma(const CacheAttn& p, int32_t grid, cudaStream_t stream);
+// bf16, head dimension 64 or 128, pages of 8, 16, 32, 64 or a multiple of 128 rows, on tcgen05; tiles of 256 rows.
+constexpr int kUmmaKeys = 128;
+bool attn_umma_supported(int32_t dh, int32_t page);
+rocs_status_t attn_umma(const CacheAttn& p, int32_t H, int32_t H_kv, int64_t N, int32_t grid, cudaStream_t stream);
 
 }  // namespace rocs

@@ -1,0 +1,530 @@
+// Attention over the paged cache on tcgen05 (bf16, heads of 64 or 128): tiles of 256 rows, two sides of 128 that share the
+// key and value blocks of 128 keys in shared memory.
+//
+// 12 warps:  0-3 and 4-7   softmax of sides A and B, a thread per row
+//            8             loads Q and the K blocks, page by page through a tensor map whose last dimension is the page
+//            9             loads the V blocks, and zeroes what the last page holds behind the slot's end
+//            10            issues the products: S = Q K^T (operands in shared memory) and O += P V (P in tensor memory)
+//
+// Tensor memory: S of both sides (128 columns each), O of both sides.  P (bf16 pairs, 64 columns) takes the place of the S
+// that it comes from; the products of a side are issued in the order P_j V_j, S_{j+1}, and run in that order, so nobody
+// waits for the columns to come free, and the arrival of S_{j+1} says that O holds everything up to P_j V_j.  While a side's
+// products run, the other side's softmax does: the products of a block pair take 2048 cycles (heads of 128) and its
+// exponentials the same, so what bounds the kernel is how well the two overlap.
+//
+// Blocks go from the last key to the first: masks (the chunk's own keys) come first, and a score that falls with distance
+// is largest there.  A row's reference is the maximum of the first block in which it sees a key and moves only when a
+// block's sum passes 2^40 (a score 2^40 times the reference's weight): the block is then done again with its own
+// maximum, O and the sum scaled.  Other blocks need no maximum.  A probability keeps its 8 bits wherever the reference is,
+// sums are fp32.  All decisions are a row's own: its bits do not depend on the other rows.
+//
+// Keys that a row does not see have weight 0; a row that comes out non-finite (0 x Inf of such a key's value, or its own
+// keys') is computed again from the keys that it does see, by its warp.
+#include <algorithm>
+
+#include "cache_attn.cuh"
+
+namespace rocs {
+namespace {
+
+using namespace ptx;
+
+constexpr int kUmmaThreads = 384;
+constexpr int kSide = 128;               // rows of a side = tensor memory lanes
+constexpr int BK = kUmmaKeys;
+constexpr uint32_t kStatusCache = 0x500;
+constexpr float kMoveAt = 1099511627776.f;  // 2^40
+
+template <int DH_>
+struct UmmaCfg {
+  static constexpr int DH = DH_;
+  static constexpr int kBoxes = DH / 64;                    // operand tiles are boxes of 64 columns, 128-byte rows
+  static constexpr int kBoxBytes = 128 * 128;               // 128 rows (queries or keys) of a box
+  static constexpr int kTileBytes = kBoxes * kBoxBytes;     // a side's Q, a K block, a V block
+  static constexpr int kStages = DH == 128 ? 2 : 4;         // of K and of V
+  static constexpr uint32_t kOffQ = 0;
+  static constexpr uint32_t kOffK = kOffQ + 2 * kTileBytes;
+  static constexpr uint32_t kOffV = kOffK + kStages * kTileBytes;
+  static constexpr uint32_t kOffBar = kOffV + kStages * kTileBytes;
+  static constexpr uint32_t kQFull = kOffBar, kQEmpty = kQFull + 8, kSFull = kQEmpty + 8, kPFull = kSFull + 16, kOFull = kPFull + 16,
+                            kTail = kOFull + 16, kDrain = kTail + 8, kKFull = kDrain + 8, kKEmpty = kKFull + 8 * kStages,
+                            kVFull = kKEmpty + 8 * kStages, kVEmpty = kVFull + 8 * kStages, kOffTmem = kVEmpty + 8 * kStages,
+                            kOffAbort = kOffTmem + 8;
+  static constexpr int kSmem = kOffAbort + 8;
+  static constexpr uint32_t kColO = 256;                    // O of side s at 256 + s * DH
+  static_assert(kSmem + (int)sizeof(AttnLine) + 1024 <= 227 * 1024, "shared memory of one SM");
+};
+
+__device__ __forceinline__ void tma_load_3d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int32_t x, int32_t y, int32_t z) {
+  asm volatile(
+      "cp.async.bulk.tensor.3d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5}], [%2];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z)
+      : "memory");
+}
+__device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map, uint32_t bar, int32_t x, int32_t y, int32_t z,
+                                            int32_t w) {
+  asm volatile(
+      "cp.async.bulk.tensor.4d.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%3, %4, %5, %6}], [%2];"
+      ::"r"(dst), "l"(reinterpret_cast<uint64_t>(map)), "r"(bar), "r"(x), "r"(y), "r"(z), "r"(w)
+      : "memory");
+}
+// D[tmem] (+)= A[tmem] * B[smem]: A holds bf16 pairs in 32-bit columns (16 keys = 8 columns).
+__device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+  asm volatile(
+      "{\n.reg .pred p;\nsetp.ne.b32 p, %4, 0;\n"
+      "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
+      "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
+__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
+  tmem_st_32x32b_x16(taddr, r);
+  tmem_st_32x32b_x16(taddr + 16, r + 16);
+}
+__device__ __forceinline__ uint64_t fadd2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+
+template <int DH, bool CAP, bool BIAS>
+__global__ void __launch_bounds__(kUmmaThreads, 1)
+umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
+            const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CacheAttn p) {
+  using C = UmmaCfg<DH>;
+  constexpr int kStages = C::kStages;
+  extern __shared__ __align__(1024) uint8_t smem[];
+  __shared__ AttnLine line_mem;
+  const uint32_t sb = smem_u32(smem);
+  AbortFlag* abort_flag = reinterpret_cast<AbortFlag*>(smem + C::kOffAbort);
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  if ((sb & 1023u) != 0) {  // the swizzled tiles assume a 1024-byte aligned base
+    if (threadIdx.x == 0) atomicCAS(p.status, 0u, kStatusCache | 15);
+    return;
+  }
+  if (threadIdx.x == 0) {
+    auto init = [&](uint32_t off, int n, uint32_t count) {
+      for (int x = 0; x < n; ++x) mbar_init(reinterpret_cast<uint64_t*>(smem + off + 8 * x), count);
+    };
+    init(C::kQFull, 1, 1);
+    init(C::kQEmpty, 1, 1);
+    init(C::kSFull, 2, 1);
+    init(C::kPFull, 2, 4);
+    init(C::kOFull, 2, 1);
+    init(C::kTail, 1, 1);
+    init(C::kDrain, 1, 1);
+    init(C::kKFull, kStages, 1);
+    init(C::kKEmpty, kStages, 1);
+    init(C::kVFull, kStages, 1);
+    init(C::kVEmpty, kStages, 1);
+    abort_flag->v = 0;
+    fence_mbar_init();
+  }
+  if (warp == 10) {
+    tmem_alloc(reinterpret_cast<uint32_t*>(smem + C::kOffTmem), 512);
+    tmem_relinquish();
+  }
+  if (warp == 8 && lane == 0) {
+    prefetch_tensormap(&map_q);
+    prefetch_tensormap(&map_k);
+    prefetch_tensormap(&map_v);
+  }
+  tc_fence_before_sync();
+  __syncthreads();
+  tc_fence_after_sync();
+  const uint32_t tmem = *reinterpret_cast<const uint32_t*>(smem + C::kOffTmem);
+  griddep_wait();
+  griddep_launch_dependents();
+  const AttnLineView view = attn_line<kUmmaThreads>(p, line_mem);
+  AttnWalk walk;
+  const bool any = walk.start(p, view);
+  const int32_t per_side = p.rows_per_tile / 2;  // batch rows of a side
+
+  if (!any) {
+    // no work: straight to the end
+  } else if (warp == 8 || warp == 9) {
+    // ------------------------------ loads ------------------------------------------------------
+    const bool is_k = warp == 8;
+    const CUtensorMap* map = is_k ? &map_k : &map_v;
+    const uint32_t full = sb + (is_k ? C::kKFull : C::kVFull), empty = sb + (is_k ? C::kKEmpty : C::kVEmpty);
+    const uint32_t dst0 = sb + (is_k ? C::kOffK : C::kOffV);
+    const int32_t box_rows = min(p.page, BK), boxes = BK / box_rows;  // pages (or parts of one) of a block
+    uint32_t it = 0, n_piece = 0, n_tail = 0;
+    bool ok = true;
+    auto wait = [&](uint32_t bar, uint32_t parity, uint32_t code) {
+      return __all_sync(0xffffffffu, mbar_wait_paced(bar, parity, abort_flag, p.status, kStatusCache | code)) != 0;
+    };
+    for (; ok && walk.more(); walk.next(p, view)) {
+      const AttnEntry e = view.entry[walk.entry];
+      if (e.blocks == 0) continue;
+      const int32_t blk0 = e.blk0 + walk.block0(), n = walk.blocks(), kv_head = walk.head / p.per_kv;
+      const int32_t* row = p.table + (int64_t)e.slot * p.width;
+      auto look_up = [&](int32_t b) {  // page of this lane's box of block b; none behind the slot's end: zeros
+        const int32_t j = (blk0 + b) * BK + lane * box_rows;
+        return lane < boxes && j < e.L ? row[page_of(p, j)] : -1;
+      };
+      int32_t id_next = look_up(n - 1);
+      if (is_k) {
+        if (!wait(sb + C::kQEmpty, (n_piece & 1) ^ 1, 1)) { ok = false; break; }
+        const int sides = e.count > per_side ? 2 : 1;
+        if (elect_one()) {
+          const uint32_t bytes = (uint32_t)(per_side * p.group) * 128u * C::kBoxes;
+          mbar_expect_tx(sb + C::kQFull, sides * bytes);
+          for (int s = 0; s < sides; ++s)
+#pragma unroll
+            for (int bx = 0; bx < C::kBoxes; ++bx)
+              tma_load_3d(sb + C::kOffQ + s * C::kTileBytes + bx * C::kBoxBytes, &map_q, sb + C::kQFull, bx * 64, walk.head * p.group,
+                          e.row0 + s * per_side);
+        }
+        __syncwarp();
+      }
+      ++n_piece;
+      for (int32_t b = n - 1; b >= 0; --b) {
+        const int32_t id = id_next;
+        if (b > 0) id_next = look_up(b - 1);
+        const uint32_t st = it % kStages;
+        if (!wait(empty + 8 * st, ((it / kStages) & 1) ^ 1, is_k ? 2 : 3)) { ok = false; break; }
+        const int32_t j0 = (blk0 + b) * BK;
+        const int32_t in_page = p.page > BK ? j0 - page_of(p, j0) * p.page : 0;
+        // what the slot's last page holds behind its end may be anything, and 0 x NaN is not 0: such a V block lands on a
+        // barrier of the loader's own, which zeroes the rest of the page and then passes the block on
+        const bool tail = !is_k && j0 + BK > e.L && e.L % p.page != 0;
+        const uint32_t landed = tail ? sb + C::kTail : full + 8 * st;
+        if (lane == 0) mbar_expect_tx(landed, C::kTileBytes);
+        __syncwarp();
+        for (int32_t x = 0; x < boxes; ++x) {
+          const int32_t page = __shfl_sync(0xffffffffu, id, x);
+          if (elect_one()) {
+#pragma unroll
+            for (int bx = 0; bx < C::kBoxes; ++bx)
+              tma_load_4d(dst0 + st * C::kTileBytes + bx * C::kBoxBytes + x * box_rows * 128, map, landed, bx * 64, in_page, kv_head,
+                          page);
+          }
+          __syncwarp();
+        }
+        if (tail) {
+          if (!wait(landed, n_tail & 1, 4)) { ok = false; break; }
+          ++n_tail;
+          const int32_t first = e.L - j0, last = min((e.L + p.page - 1) / p.page * p.page - j0, BK);
+          uint8_t* v = smem + C::kOffV + st * C::kTileBytes;
+          for (int bx = 0; bx < C::kBoxes; ++bx)
+            for (int32_t x = first * 8 + lane; x < last * 8; x += 32)
+              *reinterpret_cast<uint4*>(v + bx * C::kBoxBytes + x * 16) = make_uint4(0u, 0u, 0u, 0u);
+          fence_proxy_async_smem();
+          __syncwarp();
+          if (lane == 0) mbar_arrive(full + 8 * st);
+        }
+        ++it;
+      }
+    }
+    if (!ok) {  // let the loads in flight land before the CTA's shared memory goes away
+      for (uint32_t s = 0; s < kStages; ++s) {
+        const uint32_t issued = it / kStages + ((it % kStages > s) ? 1 : 0);
+        if (issued == 0) continue;
+        const uint64_t t0 = globaltimer_ns();
+        while (!mbar_try_wait_brief(full + 8 * s, (issued - 1) & 1) && globaltimer_ns() - t0 < kWaitLimitNs) {}
+      }
+      if (is_k && n_piece > 0) {
+        const uint64_t t0 = globaltimer_ns();
+        while (!mbar_try_wait_brief(sb + C::kQFull, (n_piece - 1) & 1) && globaltimer_ns() - t0 < kWaitLimitNs) {}
+      }
+    }
+  } else if (warp == 10) {
+    // ------------------------------ products: one thread ---------------------------------------
+    if (elect_one()) {
+      constexpr uint32_t idesc_s = umma_idesc_bf16(kSide, BK, false, false);  // S = Q K^T, both K-major
+      constexpr uint32_t idesc_o = umma_idesc_bf16(kSide, DH, false, true);   // O = P V, V is MN-major
+      const uint64_t dq = smem_desc_sw128(sb + C::kOffQ, 1024, 16);
+      const uint64_t dk = smem_desc_sw128(sb + C::kOffK, 1024, 16);
+      const uint64_t dv = smem_desc_sw128(sb + C::kOffV, 1024, C::kBoxes > 1 ? C::kBoxBytes : 16);
+      uint32_t kt = 0, vt = 0, n_piece = 0, cnt_p[2] = {0, 0};
+      bool ok = true;
+      auto wait = [&](uint32_t bar, uint32_t parity, uint32_t code) {
+        if (!mbar_wait_paced(bar, parity, abort_flag, p.status, kStatusCache | code)) ok = false;
+        return ok;
+      };
+      auto issue_s = [&](int side, uint32_t st) {
+#pragma unroll
+        for (int k = 0; k < DH / 16; ++k)
+          umma_ss(tmem + side * 128, dq + side * (C::kTileBytes >> 4) + (k / 4) * (C::kBoxBytes >> 4) + 2 * (k % 4),
+                  dk + st * (C::kTileBytes >> 4) + (k / 4) * (C::kBoxBytes >> 4) + 2 * (k % 4), idesc_s, k != 0 ? 1u : 0u);
+        umma_commit(sb + C::kSFull + 8 * side);
+      };
+      auto issue_pv = [&](int side, uint32_t st, bool first) {
+#pragma unroll
+        for (int k = 0; k < BK / 16; ++k)
+          umma_ts(tmem + C::kColO + side * DH, tmem + side * 128 + k * 8, dv + st * (C::kTileBytes >> 4) + k * (16 * 128 / 16), idesc_o,
+                  first && k == 0 ? 0u : 1u);
+      };
+      for (; ok && walk.more(); walk.next(p, view)) {
+        const AttnEntry e = view.entry[walk.entry];
+        if (e.blocks == 0) continue;
+        const int32_t n = walk.blocks();
+        const int sides = e.count > per_side ? 2 : 1;
+        if (!wait(sb + C::kQFull, n_piece & 1, 5)) break;
+        ++n_piece;
+        if (!wait(sb + C::kKFull + 8 * (kt % kStages), (kt / kStages) & 1, 6)) break;
+        tc_fence_after_sync();
+        for (int s = 0; s < sides; ++s) issue_s(s, kt % kStages);
+        umma_commit(sb + C::kKEmpty + 8 * (kt % kStages));
+        ++kt;
+        if (n == 1) umma_commit(sb + C::kQEmpty);
+        for (int32_t b = 0; b < n && ok; ++b) {
+          const uint32_t vs = vt % kStages;
+          for (int s = 0; s < sides; ++s) {
+            if (!wait(sb + C::kPFull + 8 * s, cnt_p[s] & 1, 7)) break;
+            ++cnt_p[s];
+            if (s == 0) {
+              if (!wait(sb + C::kVFull + 8 * vs, (vt / kStages) & 1, 8)) break;
+              if (b + 1 < n && !wait(sb + C::kKFull + 8 * (kt % kStages), (kt / kStages) & 1, 6)) break;
+            }
+            tc_fence_after_sync();
+            issue_pv(s, vs, b == 0);
+            if (b + 1 < n) issue_s(s, kt % kStages);
+            else umma_commit(sb + C::kOFull + 8 * s);
+          }
+          if (!ok) break;
+          umma_commit(sb + C::kVEmpty + 8 * vs);
+          ++vt;
+          if (b + 1 < n) {
+            umma_commit(sb + C::kKEmpty + 8 * (kt % kStages));
+            ++kt;
+            if (b + 2 == n) umma_commit(sb + C::kQEmpty);  // the piece's last S
+          }
+        }
+      }
+      if (!ok) {
+        umma_commit(sb + C::kDrain);
+        const uint64_t t0 = globaltimer_ns();
+        while (!mbar_try_wait_brief(sb + C::kDrain, 0) && globaltimer_ns() - t0 < kWaitLimitNs) {}
+      }
+    }
+  } else if (warp < 8) {
+    // ------------------------------ softmax ----------------------------------------------------
+    const int side = warp / 4;
+    const int row = (warp % 4) * 32 + lane;  // of the side
+    const uint32_t t_lane = tmem + ((uint32_t)((warp % 4) * 32) << 16);
+    const uint32_t t_s = t_lane + side * 128, t_o = t_lane + C::kColO + side * DH;
+    uint32_t cnt_s = 0, cnt_o = 0;
+    const int32_t side_rows = per_side * p.group;
+    for (; walk.more(); walk.next(p, view)) {
+      const AttnEntry e = view.entry[walk.entry];
+      if (side == 1 && e.count <= per_side) continue;
+      const int32_t t = side * per_side + row / p.group, h = walk.head * p.group + row % p.group;
+      const bool there = row < side_rows && t < e.count;
+      RowKeys keys{0, 0, 0};
+      float slope = 0.f;
+      if (there) {
+        keys = attn_row(p, e, t);
+        if (BIAS) slope = slope_of(p, h);
+      }
+      const bool sees = there && keys.lo < keys.hi;
+      uint8_t* out = p.O + (int64_t)(e.row0 + t) * p.o_row_bytes + h * p.o_head_bytes;
+      if (e.blocks == 0) {  // nobody sees a key
+        if (there)
+#pragma unroll
+          for (int c = 0; c < DH / 8; ++c) reinterpret_cast<uint4*>(out)[c] = make_uint4(0u, 0u, 0u, 0u);
+        continue;
+      }
+      // rows that do not exist ask for no mask
+      const int32_t lo_most = __reduce_max_sync(0xffffffffu, there ? keys.lo : 0);
+      const int32_t hi_least = __reduce_min_sync(0xffffffffu, there ? keys.hi : 0x7fffffff);
+      const int32_t blk0 = e.blk0 + walk.block0(), n = walk.blocks();
+      float m = sees ? -INFINITY : 0.f, l = 0.f;  // -inf: no reference yet
+      bool aborted = false;
+      for (int32_t b = n - 1; b >= 0; --b) {
+        if (!mbar_wait_paced(sb + C::kSFull + 8 * side, cnt_s & 1, abort_flag, p.status, kStatusCache | 10)) { aborted = true; break; }
+        ++cnt_s;
+        tc_fence_after_sync();
+        const int32_t j0 = (blk0 + b) * BK;
+        const bool full = j0 >= lo_most && j0 + BK <= hi_least;
+        // scores of columns c0.. of the row in log2 units but for the plain scale, -inf where the row does not see the key
+        auto scores = [&](int c0, uint32_t (&s)[32]) {
+          if (CAP || BIAS) {
+#pragma unroll
+            for (int x = 0; x < 32; ++x) {
+              float v = __uint_as_float(s[x]) * p.scale;
+              if (CAP) v = p.cap * tanh_fast(v);
+              if (BIAS) v = fmaf(-slope, fabsf((float)(keys.pos - j0 - c0 - x)), v);
+              s[x] = __float_as_uint(v);
+            }
+          }
+          if (!full) {
+            const int32_t lo = keys.lo - j0 - c0, hi = keys.hi - j0 - c0;
+#pragma unroll
+            for (int x = 0; x < 32; ++x)
+              if (x < lo || x >= hi) s[x] = 0xff800000u;
+          }
+        };
+        const float scale = CAP || BIAS ? 1.f : p.scale;
+        bool slow = __any_sync(0xffffffffu, m == -INFINITY), moves = m == -INFINITY;
+        uint32_t pk[64];
+        float sum;
+        while (true) {
+          if (slow) {
+            float mx = -INFINITY;
+#pragma unroll 1
+            for (int c = 0; c < BK; c += 32) {
+              uint32_t s[32];
+              tmem_ld_32x32b_x32(t_s + c, s);
+              tmem_ld_wait();
+              scores(c, s);
+#pragma unroll
+              for (int x = 0; x < 32; ++x) mx = fmaxf(mx, __uint_as_float(s[x]));
+            }
+            mx *= scale;
+            const float m_new = moves ? fmaxf(m, mx) : m;
+            const float a = m_new == m ? 1.f : ex2_approx(m - m_new);
+            m = m_new;
+            l *= a;
+            if (b != n - 1 && __any_sync(0xffffffffu, a != 1.f)) {
+#pragma unroll 1
+              for (int c = 0; c < DH; c += 32) {
+                uint32_t o[32];
+                tmem_ld_32x32b_x32(t_o + c, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * a);
+                tmem_st_x32(t_o + c, o);
+              }
+              tmem_st_wait();
+            }
+          }
+          const float ref = m == -INFINITY ? 0.f : m;
+          const uint64_t c2 = pack2(scale, scale), m2 = pack2(-ref, -ref);
+          uint64_t sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
+#pragma unroll
+          for (int c = 0; c < BK; c += 32) {
+            uint32_t s[32];
+            tmem_ld_32x32b_x32(t_s + c, s);
+            tmem_ld_wait();
+            scores(c, s);
+#pragma unroll
+            for (int x = 0; x < 32; x += 2) {
+              float x0, x1;
+              unpack2(ffma2(pack2(__uint_as_float(s[x]), __uint_as_float(s[x + 1])), c2, m2), x0, x1);
+              const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+              sum2[(x / 2) % 2] = fadd2(sum2[(x / 2) % 2], pack2(p0, p1));
+              pk[(c + x) / 2] = bf16_pair(p0, p1);
+            }
+          }
+          float s0, s1;
+          unpack2(fadd2(sum2[0], sum2[1]), s0, s1);
+          sum = s0 + s1;
+          moves = sees && !(sum <= kMoveAt);
+          if (slow || !__any_sync(0xffffffffu, moves)) break;
+          slow = true;
+        }
+        l += sum;
+        tmem_st_x32(t_s, pk);
+        tmem_st_x32(t_s + 32, pk + 32);
+        tmem_st_wait();
+        tc_fence_before_sync();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(sb + C::kPFull + 8 * side);
+      }
+      if (aborted) break;
+      if (!mbar_wait_paced(sb + C::kOFull + 8 * side, cnt_o & 1, abort_flag, p.status, kStatusCache | 11)) break;
+      ++cnt_o;
+      tc_fence_after_sync();
+      const bool whole = walk.whole();
+      const int32_t part = walk.part(), tile_row = side * side_rows + row;
+      const float inv = sees ? 1.f / l : 0.f;
+      float probe = l * 0.f;
+      float* to = attn_part(p, part) + (int64_t)tile_row * DH;
+#pragma unroll
+      for (int c = 0; c < DH; c += 32) {
+        uint32_t o[32];
+        tmem_ld_32x32b_x32(t_o + c, o);
+        tmem_ld_wait();
+#pragma unroll
+        for (int x = 0; x < 32; ++x) probe = fmaf(__uint_as_float(o[x]), 0.f, probe);
+        if (!there) continue;
+        if (whole) {
+#pragma unroll
+          for (int x = 0; x < 32; x += 8) {
+            uint4 w;
+            w.x = bf16_pair(__uint_as_float(o[x]) * inv, __uint_as_float(o[x + 1]) * inv);
+            w.y = bf16_pair(__uint_as_float(o[x + 2]) * inv, __uint_as_float(o[x + 3]) * inv);
+            w.z = bf16_pair(__uint_as_float(o[x + 4]) * inv, __uint_as_float(o[x + 5]) * inv);
+            w.w = bf16_pair(__uint_as_float(o[x + 6]) * inv, __uint_as_float(o[x + 7]) * inv);
+            *reinterpret_cast<uint4*>(out + (c + x) * 2) = w;
+          }
+        } else {
+#pragma unroll
+          for (int x = 0; x < 32; x += 4)
+            *reinterpret_cast<float4*>(to + c + x) = make_float4(__uint_as_float(o[x]), __uint_as_float(o[x + 1]), __uint_as_float(o[x + 2]),
+                                                                 __uint_as_float(o[x + 3]));
+        }
+      }
+      if (there && !whole) attn_part_sums(p, gridDim.x, part)[tile_row] = make_float2(m, l);
+      tc_fence_before_sync();  // the next piece's first P V overwrites O
+      uint32_t bad = __ballot_sync(0xffffffffu, there && probe != 0.f);
+      __syncwarp();
+      while (bad != 0) {  // a row at a time, by the warp
+        const int src = __ffs(bad) - 1;
+        bad &= bad - 1;
+        const int32_t r = (warp % 4) * 32 + src, rt = side * per_side + r / p.group, rh = walk.head * p.group + r % p.group;
+        const RowKeys rk = attn_row(p, e, rt);
+        float acc[DH / 32], mm, ll;
+        attn_row_by_hand<DH>(p, e, (int64_t)(walk.head / p.per_kv) * p.head_bytes,
+                             p.Q + (int64_t)(e.row0 + rt) * p.q_row_bytes + rh * p.q_head_bytes, rk, slope_of(p, rh), blk0 * BK,
+                             (blk0 + n) * BK, mm, ll, acc);
+        if (whole) {
+          __nv_bfloat16* o = reinterpret_cast<__nv_bfloat16*>(p.O + (int64_t)(e.row0 + rt) * p.o_row_bytes + rh * p.o_head_bytes);
+#pragma unroll
+          for (int c = 0; c < DH / 32; ++c) o[lane + 32 * c] = __float2bfloat16_rn(rk.lo < rk.hi ? acc[c] / ll : 0.f);
+        } else {
+          float* o = attn_part(p, part) + (int64_t)(side * side_rows + r) * DH;
+#pragma unroll
+          for (int c = 0; c < DH / 32; ++c) o[lane + 32 * c] = acc[c];
+          if (lane == 0) attn_part_sums(p, gridDim.x, part)[side * side_rows + r] = make_float2(mm, ll);
+        }
+      }
+    }
+  }
+
+  tc_fence_before_sync();
+  __syncthreads();
+  if (warp == 10) {
+    tc_fence_after_sync();
+    tmem_dealloc(tmem, 512);
+  }
+}
+
+template <int DH, bool CAP, bool BIAS>
+rocs_status_t launch_umma(const CacheAttn& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int32_t grid,
+                          cudaStream_t stream) {
+  auto kernel = umma_kernel<DH, CAP, BIAS>;
+  ROCS_ALLOW_SMEM(kernel, UmmaCfg<DH>::kSmem);
+  return launch_dependent(kernel, dim3((unsigned)grid), kUmmaThreads, (size_t)UmmaCfg<DH>::kSmem, stream, q, k, v, p);
+}
+template <int DH>
+rocs_status_t umma_of(const CacheAttn& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int32_t grid,
+                      cudaStream_t stream) {
+  if (p.cap > 0.f) return p.slopes ? launch_umma<DH, true, true>(p, q, k, v, grid, stream) : launch_umma<DH, true, false>(p, q, k, v, grid, stream);
+  return p.slopes ? launch_umma<DH, false, true>(p, q, k, v, grid, stream) : launch_umma<DH, false, false>(p, q, k, v, grid, stream);
+}
+
+}  // namespace
+
+bool attn_umma_supported(int32_t dh, int32_t page) {
+  return (dh == 64 || dh == 128) && (page % BK == 0 || page == 64 || page == 32 || page == 16 || page == 8);
+}
+
+rocs_status_t attn_umma(const CacheAttn& p, int32_t H, int32_t H_kv, int64_t N, int32_t grid, cudaStream_t stream) {
+  // a dimension of one entry keeps a stride that a tensor map takes
+  const uint64_t dh = (uint64_t)p.dh, dense = dh * 2;
+  auto stride = [&](int64_t bytes) { return bytes > 0 ? (uint64_t)bytes : dense; };
+  CUtensorMap q, k, v;
+  const uint64_t q_dims[3] = {dh, (uint64_t)H, (uint64_t)N}, q_strides[2] = {stride(H > 1 ? p.q_head_bytes : 0), stride(N > 1 ? p.q_row_bytes : 0)};
+  const uint32_t q_box[3] = {64, (uint32_t)p.group, (uint32_t)(p.rows_per_tile / 2)};
+  const uint64_t dims[4] = {dh, (uint64_t)p.page, (uint64_t)H_kv, (uint64_t)p.n_pages};
+  const uint64_t strides[3] = {stride(p.token_bytes), stride(p.head_bytes), stride(p.page_bytes)};
+  const uint32_t box[4] = {64, (uint32_t)std::min(p.page, BK), 1, 1};
+  if (!make_tensor_map_bf16(&q, p.Q, 3, q_dims, q_strides, q_box) || !make_tensor_map_bf16(&k, p.K, 4, dims, strides, box) ||
+      !make_tensor_map_bf16(&v, p.V, 4, dims, strides, box))
+    return ROCS_ERR_CUDA;
+  return p.dh == 128 ? umma_of<128>(p, q, k, v, grid, stream) : umma_of<64>(p, q, k, v, grid, stream);
+}
+
+}  // namespace rocs
