@@ -60,55 +60,50 @@ __device__ __forceinline__ void store_row(uint8_t* out, int32_t c, float v) {
   else reinterpret_cast<__nv_bfloat16*>(out)[c] = __float2bfloat16_rn(v);
 }
 
-// Joins the parts of the tiles that a cut went through: O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i with M the
-// largest reference, part by part in the order of the keys.  A warp per row, its lanes 32 parts' weights first and output
-// columns then; blockIdx.x is the cut.
+// Joins the parts of the tiles that a cut went through: O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i, part by part in
+// the order of the keys with the largest reference so far as M.  A warp per row, lanes are output columns; blockIdx.x is the
+// cut.  Four parts are fetched at once: the kernel is a few trips to memory long.
 constexpr int kJoinThreads = 128;
 template <typename T, int NV>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(CacheAttn p, int32_t grid) {
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const AttnMeta m = p.meta[blockIdx.x];
-  if (m.end == 0) return;
-  const int64_t total = p.header[0];
-  const int32_t ctas = (int32_t)p.header[1];
-  const AttnEntry e = p.listed ? p.entries_global[m.entry] : attn_entry(p, m.entry);
+  if (m.parts == 0) return;
+  const AttnEntry& e = m.entry;
   const int lane = threadIdx.x % 32;
-  const int32_t b0 = (int32_t)blockIdx.x - 1;
-  int32_t parts = 1;
-  while (b0 + parts < ctas && AttnWalk::cut(total, ctas, b0 + parts) < m.end) ++parts;
-  const bool first_of_cta = AttnWalk::cut(total, ctas, b0) == m.begin;
-  auto place = [&](int32_t i) { return 2 * (b0 + i) + (i == 0 && !first_of_cta ? 1 : 0); };
+  auto place = [&](int32_t i) { return i == 0 ? m.place : 2 * ((int32_t)blockIdx.x - 1 + i); };
   const int32_t rows = e.count * p.group;
   for (int32_t row = blockIdx.y * (kJoinThreads / 32) + threadIdx.x / 32; row < rows; row += gridDim.y * (kJoinThreads / 32)) {
-    float M = -INFINITY;
-    for (int32_t i = lane; i < parts; i += 32) M = fmaxf(M, attn_part_sums(p, grid, place(i))[row].x);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) M = fmaxf(M, __shfl_xor_sync(0xffffffffu, M, o));
-    float acc[NV], l = 0.f;
+    float M = -INFINITY, l = 0.f, acc[NV];
 #pragma unroll
     for (int c = 0; c < NV; ++c) acc[c] = 0.f;
-    for (int32_t i0 = 0; i0 < parts; i0 += 32) {
-      float w = 0.f;
-      if (i0 + lane < parts) {
-        const float2 s = attn_part_sums(p, grid, place(i0 + lane))[row];
-        // a part in which the row saw no key, or only scores of -inf, adds nothing
-        w = s.x == -INFINITY && s.y == 0.f ? 0.f : exp2f((s.x - M) * p.unit);
-        l += s.y == 0.f ? 0.f : w * s.y;
-      }
-      const int32_t here = min(parts - i0, 32);
-#pragma unroll 4
-      for (int32_t k = 0; k < here; ++k) {
-        const float wk = __shfl_sync(0xffffffffu, w, k);
-        if (wk == 0.f) continue;
-        const float* o = attn_part(p, place(i0 + k)) + (int64_t)row * p.dh;
+    for (int32_t i0 = 0; i0 < m.parts; i0 += 4) {
+      float2 s[4];
+      float o[4][NV];
 #pragma unroll
-        for (int c = 0; c < NV; ++c)
-          if (lane + 32 * c < p.dh) acc[c] = fmaf(wk, o[lane + 32 * c], acc[c]);
+      for (int k = 0; k < 4; ++k) {
+        s[k] = make_float2(-INFINITY, 0.f);
+        if (i0 + k >= m.parts) continue;
+        s[k] = attn_part_sums(p, grid, place(i0 + k))[row];
+        const float* from = attn_part(p, place(i0 + k)) + (int64_t)row * p.dh;
+#pragma unroll
+        for (int c = 0; c < NV; ++c) o[k][c] = lane + 32 * c < p.dh ? from[lane + 32 * c] : 0.f;
+      }
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        // a part in which the row saw no key, or only scores of -inf, adds nothing (its sum is 0, or NaN)
+        if (s[k].x == -INFINITY) {
+          l += s[k].y;
+          continue;
+        }
+        const float M_new = fmaxf(M, s[k].x), a = M == M_new ? 1.f : exp2f((M - M_new) * p.unit), w = exp2f((s[k].x - M_new) * p.unit);
+        M = M_new;
+        l = fmaf(l, a, w * s[k].y);
+#pragma unroll
+        for (int c = 0; c < NV; ++c) acc[c] = fmaf(acc[c], a, w * o[k][c]);
       }
     }
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) l += __shfl_xor_sync(0xffffffffu, l, o);
     const int32_t t = row / p.group;
     const RowKeys keys = attn_row(p, e, t);
     uint8_t* out = p.O + (int64_t)(e.row0 + t) * p.o_row_bytes + (m.head * p.group + row % p.group) * p.o_head_bytes;
@@ -120,7 +115,7 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(CacheAttn p, int32_t
 
 template <typename T>
 rocs_status_t join_parts(const CacheAttn& p, int32_t grid, cudaStream_t stream) {
-  const dim3 blocks((unsigned)grid, (unsigned)std::min(p.tile_rows / 4, 16));
+  const dim3 blocks((unsigned)grid, (unsigned)(p.tile_rows / 4));
   if (p.dh <= 64) return launch_dependent(join_kernel<T, 2>, blocks, kJoinThreads, 0, stream, p, grid);
   if (p.dh <= 128) return launch_dependent(join_kernel<T, 4>, blocks, kJoinThreads, 0, stream, p, grid);
   return launch_dependent(join_kernel<T, 8>, blocks, kJoinThreads, 0, stream, p, grid);
@@ -333,7 +328,7 @@ int sm_count() {
   return n;
 }
 
-enum class Kind { kGeneral, kMma, kUmma };
+enum class Kind { kGeneral, kMma, kFew, kUmma };
 
 // Which kernel a call takes, and how its work is cut.
 struct Choice {
@@ -354,6 +349,10 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H) {
     x.kind = Kind::kMma;
     x.block = kMmaKeys;
     if ((int64_t)plan->largest * g > 16) most = 64;
+    else if (attn_few_supported(c->dh, c->page)) {
+      x.kind = Kind::kFew;
+      x.block = kFewKeys;
+    }
     if ((int64_t)plan->largest * g > 64 && attn_umma_supported(c->dh, c->page)) {
       x.kind = Kind::kUmma;
       x.block = kUmmaKeys;
@@ -362,7 +361,7 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H) {
   }
   // the CTAs of one round of the chip: 128 registers a thread, and shared memory (with the line and the probabilities)
   const int smem = (c->dtype == ROCS_BF16 ? gen_smem<__nv_bfloat16>(c->dh) : gen_smem<float>(c->dh)) + (int)sizeof(AttnLine) + 4096;
-  x.grid = sms * (x.kind == Kind::kUmma ? 1 : x.kind == Kind::kMma ? attn_mma_ctas_per_sm(c->dh) : std::min(4, 228 * 1024 / smem));
+  x.grid = sms * (x.kind == Kind::kUmma ? 1 : x.kind == Kind::kFew ? attn_few_ctas_per_sm(c->dh) : x.kind == Kind::kMma ? attn_mma_ctas_per_sm(c->dh) : std::min(4, 228 * 1024 / smem));
   x.group = 1;  // the largest part of the heads of a key head that fits a tile
   for (int32_t d = std::min(g, most); d >= 1; --d)
     if (g % d == 0) { x.group = d; break; }
@@ -381,7 +380,7 @@ struct Places {
 };
 Places places(const Choice& x, int32_t dh) {
   Places w;
-  w.meta = 256;
+  w.meta = 0;
   w.line = w.meta + round_up(sizeof(AttnMeta) * (size_t)x.grid, 256);
   w.entries = w.line + round_up(sizeof(int64_t) * ((size_t)x.entries + 1), 256);
   w.parts = w.entries + round_up(sizeof(AttnEntry) * (size_t)x.entries, 256);
@@ -470,7 +469,6 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
   p.min_units = x.min_units;
   p.tile_rows = x.tile_rows;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
-  p.header = reinterpret_cast<int64_t*>(ws);
   p.meta = reinterpret_cast<AttnMeta*>(ws + w.meta);
   p.line_global = reinterpret_cast<int64_t*>(ws + w.line);
   p.entries_global = reinterpret_cast<AttnEntry*>(ws + w.entries);
@@ -489,6 +487,7 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
     if (st != ROCS_OK) return st;
   }
   const rocs_status_t st = x.kind == Kind::kUmma  ? attn_umma(p, H, c->H_kv, plan->N, x.grid, stream)
+                           : x.kind == Kind::kFew ? attn_few(p, c->H_kv, x.grid, stream)
                            : x.kind == Kind::kMma ? attn_mma(p, x.grid, stream)
                                                   : attn_general(c->dtype, p, x.grid, stream);
   if (st != ROCS_OK) return st;

@@ -27,9 +27,11 @@ struct AttnEntry {
 };
 
 struct AttnMeta {   // of a CTA whose first piece continues a tile that the CTA in front began
-  int64_t begin, end;  // units of the tile; end 0: no such piece
-  int32_t entry, head;
-  int64_t pad;
+  AttnEntry entry;
+  int32_t head;
+  int32_t parts;    // of the tile; 0: no such piece
+  int32_t place;    // of the first of them
+  int32_t pad;
 };
 
 struct CacheAttn {
@@ -55,11 +57,19 @@ struct CacheAttn {
   int64_t* line_global;     // [entries + 1]
   AttnEntry* entries_global;
   bool listed;              // the two above were made by a launch in front
-  int64_t* header;          // [0] units of the line, [1] CTAs that share it
   AttnMeta* meta;           // [CTAs]
   float* parts;             // [2 CTAs][tile_rows][dh], then [2 CTAs][tile_rows][2]: reference and sum
   uint32_t* status;
 };
+
+// Tensor map of the layer's K or V, [pages][heads][rows of a page][dh], for blocks of `keys` keys.
+inline bool make_page_map(CUtensorMap* map, const void* base, const CacheAttn& p, int32_t H_kv, int32_t keys) {
+  auto stride = [&](int64_t bytes) { return bytes > 0 ? (uint64_t)bytes : (uint64_t)p.dh * 2; };  // a single entry has none
+  const uint64_t dims[4] = {(uint64_t)p.dh, (uint64_t)p.page, (uint64_t)H_kv, (uint64_t)p.n_pages};
+  const uint64_t strides[3] = {stride(p.token_bytes), stride(p.head_bytes), stride(p.page_bytes)};
+  const uint32_t box[4] = {p.dh == 32 ? 32u : 64u, (uint32_t)(p.page < keys ? p.page : keys), 1, 1};
+  return make_tensor_map_bf16(map, base, 4, dims, strides, box);
+}
 
 #ifdef __CUDACC__
 struct AttnLine {
@@ -153,19 +163,15 @@ struct AttnWalk {
   int32_t entry, head, cost;
   bool first;          // the piece at hand is the CTA's first
   __device__ __forceinline__ static int64_t cut(int64_t total, int32_t ctas, int32_t i) { return total * i / ctas; }
-  // false: nothing for this CTA.  CTA 0 notes what the joining kernel needs.
+  // false: nothing for this CTA.  Thread 0 notes what the joining kernel needs.
   __device__ __forceinline__ bool start(const CacheAttn& p, const AttnLineView& v) {
     const int64_t total = v.line[p.entries] * p.heads;
     const int32_t ctas = (int32_t)min((int64_t)gridDim.x, max(total / p.min_units, (int64_t)1));
     const int32_t i = blockIdx.x;
-    if (i == 0 && threadIdx.x == 0) {
-      p.header[0] = total;
-      p.header[1] = ctas;
-    }
     u = end = 0;
     first = true;
     if (i >= ctas || total == 0) {
-      if (threadIdx.x == 0) p.meta[i].end = 0;
+      if (threadIdx.x == 0) p.meta[i].parts = 0;
       return false;
     }
     u = cut(total, ctas, i);
@@ -181,12 +187,18 @@ struct AttnWalk {
     head = (int32_t)(in / cost);
     tile_begin = v.line[lo] * p.heads + (int64_t)head * cost;
     if (threadIdx.x == 0) {
-      const bool joins = u > tile_begin && cut(total, ctas, i - 1) <= tile_begin;
       AttnMeta m;
-      m.begin = tile_begin;
-      m.end = joins ? tile_begin + cost : 0;
-      m.entry = entry;
-      m.head = head;
+      m.parts = 0;
+      if (u > tile_begin) {
+        const int64_t in_front = cut(total, ctas, i - 1);
+        if (in_front <= tile_begin) {
+          m.entry = v.entry[entry];
+          m.head = head;
+          m.parts = 1;
+          while (i - 1 + m.parts < ctas && cut(total, ctas, i - 1 + m.parts) < tile_begin + cost) ++m.parts;
+          m.place = 2 * (i - 1) + (in_front == tile_begin ? 0 : 1);
+        }
+      }
       p.meta[i] = m;
     }
     return true;
@@ -325,6 +337,11 @@ rocs_status_t attn_general(rocs_dtype_t dt, const CacheAttn& p, int32_t grid, cu
 constexpr int kMmaKeys = 64;
 int attn_mma_ctas_per_sm(int32_t dh);
 rocs_status_t attn_mma(const CacheAttn& p, int32_t grid, cudaStream_t stream);
+// The same tiles of up to 16 rows with pages of 8, 16, 32 or a multiple of 64 rows: loads by tensor maps.
+constexpr int kFewKeys = 64;
+bool attn_few_supported(int32_t dh, int32_t page);
+int attn_few_ctas_per_sm(int32_t dh);
+rocs_status_t attn_few(const CacheAttn& p, int32_t H_kv, int32_t grid, cudaStream_t stream);
 // bf16, head dimension 64 or 128, pages of 8, 16, 32, 64 or a multiple of 128 rows, on tcgen05; tiles of 256 rows.
 constexpr int kUmmaKeys = 128;
 bool attn_umma_supported(int32_t dh, int32_t page);

@@ -518,11 +518,8 @@ rocs_status_t attn_umma(const CacheAttn& p, int32_t H, int32_t H_kv, int64_t N, 
   CUtensorMap q, k, v;
   const uint64_t q_dims[3] = {dh, (uint64_t)H, (uint64_t)N}, q_strides[2] = {stride(H > 1 ? p.q_head_bytes : 0), stride(N > 1 ? p.q_row_bytes : 0)};
   const uint32_t q_box[3] = {64, (uint32_t)p.group, (uint32_t)(p.rows_per_tile / 2)};
-  const uint64_t dims[4] = {dh, (uint64_t)p.page, (uint64_t)H_kv, (uint64_t)p.n_pages};
-  const uint64_t strides[3] = {stride(p.token_bytes), stride(p.head_bytes), stride(p.page_bytes)};
-  const uint32_t box[4] = {64, (uint32_t)std::min(p.page, BK), 1, 1};
-  if (!make_tensor_map_bf16(&q, p.Q, 3, q_dims, q_strides, q_box) || !make_tensor_map_bf16(&k, p.K, 4, dims, strides, box) ||
-      !make_tensor_map_bf16(&v, p.V, 4, dims, strides, box))
+  if (!make_tensor_map_bf16(&q, p.Q, 3, q_dims, q_strides, q_box) || !make_page_map(&k, p.K, p, H_kv, BK) ||
+      !make_page_map(&v, p.V, p, H_kv, BK))
     return ROCS_ERR_CUDA;
   return p.dh == 128 ? umma_of<128>(p, q, k, v, grid, stream) : umma_of<64>(p, q, k, v, grid, stream);
 }

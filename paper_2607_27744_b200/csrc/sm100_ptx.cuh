@@ -420,8 +420,8 @@ bool make_tensor_map_2d(CUtensorMap* map, const void* base, CUtensorMapDataType 
 bool make_tensor_map_3d(CUtensorMap* map, const void* base, uint64_t cols, uint64_t rows, uint64_t n, uint32_t box_cols,
                         uint32_t box_rows, uint32_t box_n);
 
-// A bf16 tensor of `rank` dimensions, the innermost dense, the others `strides` bytes apart; boxes of `box`, 64 columns wide,
-// 128-byte swizzle, zeros outside.
+// A bf16 tensor of `rank` dimensions, the innermost dense, the others `strides` bytes apart; boxes of `box`, 64 columns wide
+// (128-byte swizzle) or 32 (64-byte swizzle), zeros outside.
 bool make_tensor_map_bf16(CUtensorMap* map, const void* base, int rank, const uint64_t* dims, const uint64_t* strides,
                           const uint32_t* box);
 
