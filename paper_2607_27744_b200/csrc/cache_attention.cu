@@ -352,6 +352,7 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H) {
     else if (attn_few_supported(c->dh, c->page)) {
       x.kind = Kind::kFew;
       x.block = kFewKeys;
+      if ((int64_t)plan->largest * g <= 8) most = 8;
     }
     if ((int64_t)plan->largest * g > 64 && attn_umma_supported(c->dh, c->page)) {
       x.kind = Kind::kUmma;

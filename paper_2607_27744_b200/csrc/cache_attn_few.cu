@@ -43,7 +43,15 @@ struct FewCfg {
     if constexpr (kRowBytes == 64) return key * 64 + ((chunk ^ ((key >> 1) & 3)) << 4);
     return (chunk >> 3) * kBoxBytes + key * 128 + (((chunk & 7) ^ (key & 7)) << 4);
   }
+  // the same for chunk 2 k + c, given at(key, c): an exclusive or inside a box, and tiles begin at multiples of 1024
+  __device__ static uint32_t step(uint32_t at_c, int k) {
+    constexpr int kPerBox = kBoxCols / 16;
+    return (at_c ^ ((k % kPerBox) * 32)) + (k / kPerBox) * kBoxBytes;
+  }
 };
+
+// What stands for "no reference yet": below every score, and finite, so that it needs no case of its own.
+constexpr float kNoReference = -3.0e38f;
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
   asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0, %1, %2, %3}, [%4];"
@@ -76,8 +84,8 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* map
       : "memory");
 }
 
-// NT: groups of 8 rows (1 or 2).
-template <int DH, int NT>
+// NT: groups of 8 rows (1 or 2); MODS: scores are capped or fall with distance.
+template <int DH, int NT, bool MODS>
 __global__ void __launch_bounds__(kFewThreads, FewCfg<DH, NT>::kPerSm)
 few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CacheAttn p) {
   using C = FewCfg<DH, NT>;
@@ -168,6 +176,8 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
     ++n_meet;
     return __all_sync(0xffffffffu, ok) != 0;
   };
+  const uint32_t k_place = C::at(warp * 16 + lane % 8 + ((lane / 8) & 1) * 8, lane / 16);
+  const uint32_t v_place = C::at(warp * 16 + lane % 8 + (lane / 16) * 8, (lane / 8) & 1);
   // what a piece needs from memory, fetched while the piece in front is computed
   uint32_t q_next[NT][DH / 16][2];
   auto fetch = [&](const AttnWalk& w) {
@@ -203,7 +213,8 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
     after.next(p, view);
     fetch(after);
     // this lane's columns: rows n * 8 + 2 (lane % 4) + i
-    RowKeys keys[NT][2];
+    int32_t lo[NT][2], hi[NT][2];
+    int32_t pos[NT][2];
     float slope[NT][2], m[NT][2], l[NT][2];
     int32_t lo_most = 0, hi_least = 0x7fffffff;
 #pragma unroll
@@ -211,15 +222,18 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         const int32_t row = n * 8 + 2 * (lane % 4) + i;
-        keys[n][i] = RowKeys{0, 0x7fffffff, 0};  // a row that does not exist asks for no mask
+        RowKeys rk{0, 0x7fffffff, 0};  // a row that does not exist asks for no mask
         slope[n][i] = 0.f;
         if (row < rows) {
-          keys[n][i] = attn_row(p, e, row / p.group);
-          slope[n][i] = slope_of(p, walk.head * p.group + row % p.group);
+          rk = attn_row(p, e, row / p.group);
+          if (MODS) slope[n][i] = slope_of(p, walk.head * p.group + row % p.group);
         }
-        lo_most = max(lo_most, keys[n][i].lo);
-        hi_least = min(hi_least, keys[n][i].hi);
-        m[n][i] = -INFINITY;
+        lo[n][i] = rk.lo;
+        hi[n][i] = rk.hi;
+        pos[n][i] = rk.pos;
+        lo_most = max(lo_most, rk.lo);
+        hi_least = min(hi_least, rk.hi);
+        m[n][i] = kNoReference;
         l[n][i] = 0.f;
       }
     lo_most = __reduce_max_sync(0xffffffffu, lo_most);
@@ -249,34 +263,52 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
       for (int n = 0; n < NT; ++n)
 #pragma unroll
         for (int c = 0; c < 4; ++c) s[n][0][c] = s[n][1][c] = 0.f;
+      const uint32_t k_at = k_tile + k_place, v_at = v_tile + v_place;
 #pragma unroll
       for (int k = 0; k < DH / 16; ++k) {
         uint32_t a[4];
-        ldmatrix_x4(k_tile + C::at(key0 + lane % 8 + ((lane / 8) & 1) * 8, 2 * k + lane / 16), a);
+        ldmatrix_x4(C::step(k_at, k), a);
 #pragma unroll
         for (int n = 0; n < NT; ++n) mma_bf16(s[n][k & 1], a, q[n][k][0], q[n][k][1]);
       }
-      const bool full = j0 >= lo_most && j0 + 16 <= hi_least;
+      float x[NT][4];
+#pragma unroll
+      for (int n = 0; n < NT; ++n)
+#pragma unroll
+        for (int c = 0; c < 4; ++c) x[n][c] = (s[n][0][c] + s[n][1][c]) * p.scale;
+      if (MODS) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int i = 0; i < 2; ++i) {
+            const float away = (float)(pos[n][i] - j0 - lane / 4);
+#pragma unroll
+            for (int c = i; c < 4; c += 2) {
+              if (p.cap > 0.f) x[n][c] = p.cap * tanh_fast(x[n][c]);
+              x[n][c] = fmaf(-slope[n][i], fabsf(away - (c / 2) * 8), x[n][c]);
+            }
+          }
+      }
+      if (!(j0 >= lo_most && j0 + 16 <= hi_least)) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const int32_t j = j0 + lane / 4 + (c / 2) * 8;
+            if (j < lo[n][c % 2] || j >= hi[n][c % 2]) x[n][c] = -INFINITY;
+          }
+      }
       bool moves = false;
 #pragma unroll
       for (int n = 0; n < NT; ++n)
 #pragma unroll
-        for (int c = 0; c < 4; ++c) {
-          float x = (s[n][0][c] + s[n][1][c]) * p.scale;
-          if (p.cap > 0.f) x = p.cap * tanh_fast(x);
-          const int32_t j = j0 + lane / 4 + (c / 2) * 8;
-          const RowKeys& rk = keys[n][c % 2];
-          if (p.slopes) x -= slope[n][c % 2] * fabsf((float)(rk.pos - j));
-          if (!full && (j < rk.lo || j >= rk.hi)) x = -INFINITY;
-          s[n][0][c] = x;
-          moves |= x > m[n][c % 2] + 8.f;  // (from -inf: any score moves it)
-        }
+        for (int c = 0; c < 4; ++c) moves |= x[n][c] > m[n][c % 2] + 8.f;  // (any score passes kNoReference)
       if (__any_sync(0xffffffffu, moves)) {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
           for (int i = 0; i < 2; ++i) {
-            float mx = fmaxf(s[n][0][i], s[n][0][2 + i]);
+            float mx = fmaxf(x[n][i], x[n][2 + i]);
 #pragma unroll
             for (int d = 4; d < 32; d <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
             const float m_new = mx > m[n][i] + 8.f ? mx : m[n][i];  // a row's own decision
@@ -293,9 +325,8 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
       uint32_t pb[NT][2];
 #pragma unroll
       for (int n = 0; n < NT; ++n) {
-        const float r0 = m[n][0] == -INFINITY ? 0.f : m[n][0], r1 = m[n][1] == -INFINITY ? 0.f : m[n][1];
-        const float p0 = ex2_approx(s[n][0][0] - r0), p1 = ex2_approx(s[n][0][1] - r1), p2 = ex2_approx(s[n][0][2] - r0),
-                    p3 = ex2_approx(s[n][0][3] - r1);
+        const float p0 = ex2_approx(x[n][0] - m[n][0]), p1 = ex2_approx(x[n][1] - m[n][1]), p2 = ex2_approx(x[n][2] - m[n][0]),
+                    p3 = ex2_approx(x[n][3] - m[n][1]);
         l[n][0] += p0 + p2;
         l[n][1] += p1 + p3;
         pb[n][0] = transposed(bf16_pair(p0, p1));
@@ -311,7 +342,7 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
 #pragma unroll
       for (int t = 0; t < DH / 16; ++t) {
         uint32_t a[4];
-        ldmatrix_x4_trans(v_tile + C::at(key0 + lane % 8 + (lane / 16) * 8, 2 * t + ((lane / 8) & 1)), a);
+        ldmatrix_x4_trans(C::step(v_at, t), a);
 #pragma unroll
         for (int n = 0; n < NT; ++n) mma_bf16(o[n][t], a, pb[n][0], pb[n][1]);
       }
@@ -339,7 +370,7 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
         float ref = -INFINITY;
 #pragma unroll
         for (int w = 0; w < 4; ++w) ref = fmaxf(ref, sums[w * 16 + n * 8 + 2 * (lane % 4) + i].x);
-        f[i] = m[n][i] == -INFINITY ? 0.f : ex2_approx(m[n][i] - ref);
+        f[i] = ex2_approx(m[n][i] - ref);
       }
 #pragma unroll
       for (int u = 0; u < C::kRounds; ++u) {
@@ -373,7 +404,7 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
 #pragma unroll
         for (int w = 0; w < 4; ++w) {
           const float2 y = sums[w * 16 + row];
-          ll += y.x == -INFINITY ? y.y : ex2_approx(y.x - mm) * y.y;  // (without a reference 0, or NaN)
+          ll = fmaf(ex2_approx(y.x - mm), y.y, ll);
         }
         float probe = ll * 0.f;
 #pragma unroll
@@ -399,11 +430,17 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
   }
 }
 
-template <int DH, int NT>
+template <int DH, int NT, bool MODS>
 rocs_status_t launch_few(const CacheAttn& p, const CUtensorMap& k, const CUtensorMap& v, int32_t grid, cudaStream_t stream) {
-  auto kernel = few_kernel<DH, NT>;
+  auto kernel = few_kernel<DH, NT, MODS>;
   ROCS_ALLOW_SMEM(kernel, (FewCfg<DH, NT>::kSmem));
   return launch_dependent(kernel, dim3((unsigned)grid), kFewThreads, (size_t)FewCfg<DH, NT>::kSmem, stream, k, v, p);
+}
+template <int DH>
+rocs_status_t few_of(const CacheAttn& p, const CUtensorMap& k, const CUtensorMap& v, int32_t grid, cudaStream_t stream) {
+  const bool mods = p.cap > 0.f || p.slopes != nullptr;
+  if (p.rows_per_tile * p.group <= 8) return mods ? launch_few<DH, 1, true>(p, k, v, grid, stream) : launch_few<DH, 1, false>(p, k, v, grid, stream);
+  return mods ? launch_few<DH, 2, true>(p, k, v, grid, stream) : launch_few<DH, 2, false>(p, k, v, grid, stream);
 }
 
 }  // namespace
@@ -416,10 +453,7 @@ int attn_few_ctas_per_sm(int32_t dh) { return dh == 128 ? FewCfg<128, 2>::kPerSm
 rocs_status_t attn_few(const CacheAttn& p, int32_t H_kv, int32_t grid, cudaStream_t stream) {
   CUtensorMap k, v;
   if (!make_page_map(&k, p.K, p, H_kv, kFewKeys) || !make_page_map(&v, p.V, p, H_kv, kFewKeys)) return ROCS_ERR_CUDA;
-  const bool one = p.rows_per_tile * p.group <= 8;
-  if (p.dh == 128) return one ? launch_few<128, 1>(p, k, v, grid, stream) : launch_few<128, 2>(p, k, v, grid, stream);
-  if (p.dh == 64) return one ? launch_few<64, 1>(p, k, v, grid, stream) : launch_few<64, 2>(p, k, v, grid, stream);
-  return one ? launch_few<32, 1>(p, k, v, grid, stream) : launch_few<32, 2>(p, k, v, grid, stream);
+  return p.dh == 128 ? few_of<128>(p, k, v, grid, stream) : p.dh == 64 ? few_of<64>(p, k, v, grid, stream) : few_of<32>(p, k, v, grid, stream);
 }
 
 }  // namespace rocs
