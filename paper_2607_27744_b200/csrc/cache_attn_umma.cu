@@ -1,25 +1,26 @@
 // Attention over the paged cache on tcgen05 (bf16, heads of 64 or 128): tiles of 256 rows, two sides of 128 that share the
-// key and value blocks of 128 keys in shared memory.
+// key and value blocks of 128 keys in shared memory.  A tile of up to 128 rows has both sides on the same rows, each with
+// every other block of keys.
 //
-// 12 warps:  0-3 and 4-7   softmax of sides A and B, a thread per row
-//            8             loads Q and the K blocks, page by page through a tensor map whose last dimension is the page
-//            9             loads the V blocks, and zeroes what the last page holds behind the slot's end
-//            10            issues the products: S = Q K^T (operands in shared memory) and O += P V (P in tensor memory)
+// 20 warps:  0-7 and 8-15  softmax of sides A and B, two threads per row: each has 64 of a block's 128 columns
+//            16            loads Q and the K blocks, page by page through a tensor map whose last dimension is the page
+//            17            loads the V blocks, and zeroes what the last page holds behind the slot's end
+//            18            issues the products: S = Q K^T (operands in shared memory) and O += P V (P in tensor memory)
 //
-// Tensor memory: S of both sides (128 columns each), O of both sides.  P (bf16 pairs, 64 columns) takes the place of the S
-// that it comes from; the products of a side are issued in the order P_j V_j, S_{j+1}, and run in that order, so nobody
-// waits for the columns to come free, and the arrival of S_{j+1} says that O holds everything up to P_j V_j.  While a side's
-// products run, the other side's softmax does: the products of a block pair take 2048 cycles (heads of 128) and its
-// exponentials the same, so what bounds the kernel is how well the two overlap.
+// Tensor memory: S of both sides (128 columns each), O of both sides.  P (bf16 pairs) takes the place of the S that it comes
+// from, each half of a row in its own half of the columns; the products of a side are issued in the order P_j V_j, S_{j+1},
+// and run in that order, so nobody waits for the columns to come free, and the arrival of S_{j+1} says that O holds
+// everything up to P_j V_j.  While a side's products run, the other side's softmax does: the products of a block pair take
+// 2048 cycles (heads of 128) and its exponentials the same, so what bounds the kernel is how well the two overlap.
 //
 // Blocks go from the last key to the first: masks (the chunk's own keys) come first, and a score that falls with distance
-// is largest there.  A row's reference is the maximum of the first block in which it sees a key and moves only when a
-// block's sum passes 2^40 (a score 2^40 times the reference's weight): the block is then done again with its own
-// maximum, O and the sum scaled.  Other blocks need no maximum.  A probability keeps its 8 bits wherever the reference is,
-// sums are fp32.  All decisions are a row's own: its bits do not depend on the other rows.
+// is largest there.  A row's reference is the maximum of the first block in which it sees a key; other blocks need no
+// maximum.  It moves up where a block's sum passes 2^40, by that sum's exponent, before the next block: both threads of the
+// row read what the other's half summed to, and scale O and their sums by the same power of two.  A probability keeps its
+// 8 bits wherever the reference is, sums are fp32.  All decisions are a row's own: its bits do not depend on other rows.
 //
-// Keys that a row does not see have weight 0; a row that comes out non-finite (0 x Inf of such a key's value, or its own
-// keys') is computed again from the keys that it does see, by its warp.
+// A row whose scores pass its reference by more than fp32's range within one block, or whose masked keys hold NaN or Inf
+// values (weight 0, but 0 x Inf is not 0), comes out non-finite and is computed again from the keys that it sees, by a warp.
 #include <algorithm>
 
 #include "cache_attn.cuh"
@@ -29,7 +30,8 @@ namespace {
 
 using namespace ptx;
 
-constexpr int kUmmaThreads = 384;
+constexpr int kSoftmaxWarps = 16, kLoadK = 16, kLoadV = 17, kIssue = 18;
+constexpr int kUmmaThreads = 20 * 32;
 constexpr int kSide = 128;               // rows of a side = tensor memory lanes
 constexpr int BK = kUmmaKeys;
 constexpr uint32_t kStatusCache = 0x500;
@@ -45,9 +47,13 @@ struct UmmaCfg {
   static constexpr uint32_t kOffQ = 0;
   static constexpr uint32_t kOffK = kOffQ + 2 * kTileBytes;
   static constexpr uint32_t kOffV = kOffK + kStages * kTileBytes;
-  static constexpr uint32_t kOffBar = kOffV + kStages * kTileBytes;
+  static constexpr uint32_t kOffSum = kOffV + kStages * kTileBytes;   // [2 parities][2 sides][2 halves][128] sums of a block
+  static constexpr uint32_t kOffMax = kOffSum + 8 * kSide * 4;        // [2 sides][2 halves][128] maxima of a block
+  static constexpr uint32_t kOffEnd = kOffMax + 4 * kSide * 4;        // [2 sides][2 halves][128] (reference, sum, probe, -)
+  static constexpr uint32_t kOffBar = kOffEnd + 4 * kSide * 16;
   static constexpr uint32_t kQFull = kOffBar, kQEmpty = kQFull + 8, kSFull = kQEmpty + 8, kPFull = kSFull + 16, kOFull = kPFull + 16,
-                            kTail = kOFull + 16, kDrain = kTail + 8, kKFull = kDrain + 8, kKEmpty = kKFull + 8 * kStages,
+                            kTail = kOFull + 16, kDrain = kTail + 8, kPair = kDrain + 8, kQuad = kPair + 64, kKFull = kQuad + 32,
+                            kKEmpty = kKFull + 8 * kStages,
                             kVFull = kKEmpty + 8 * kStages, kVEmpty = kVFull + 8 * kStages, kOffTmem = kVEmpty + 8 * kStages,
                             kOffAbort = kOffTmem + 8;
   static constexpr int kSmem = kOffAbort + 8;
@@ -75,10 +81,6 @@ __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64
       "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, p;\n}\n" ::"r"(d_tmem),
       "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
-}
-__device__ __forceinline__ void tmem_st_x32(uint32_t taddr, const uint32_t* r) {
-  tmem_st_32x32b_x16(taddr, r);
-  tmem_st_32x32b_x16(taddr + 16, r + 16);
 }
 __device__ __forceinline__ uint64_t fadd2(uint64_t a, uint64_t b) {
   uint64_t d;
@@ -108,10 +110,12 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
     init(C::kQFull, 1, 1);
     init(C::kQEmpty, 1, 1);
     init(C::kSFull, 2, 1);
-    init(C::kPFull, 2, 4);
+    init(C::kPFull, 2, 8);
     init(C::kOFull, 2, 1);
     init(C::kTail, 1, 1);
     init(C::kDrain, 1, 1);
+    init(C::kPair, 8, 2);
+    init(C::kQuad, 4, 4);
     init(C::kKFull, kStages, 1);
     init(C::kKEmpty, kStages, 1);
     init(C::kVFull, kStages, 1);
@@ -119,11 +123,11 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
     abort_flag->v = 0;
     fence_mbar_init();
   }
-  if (warp == 10) {
+  if (warp == kIssue) {
     tmem_alloc(reinterpret_cast<uint32_t*>(smem + C::kOffTmem), 512);
     tmem_relinquish();
   }
-  if (warp == 8 && lane == 0) {
+  if (warp == kLoadK && lane == 0) {
     prefetch_tensormap(&map_q);
     prefetch_tensormap(&map_k);
     prefetch_tensormap(&map_v);
@@ -141,9 +145,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
 
   if (!any) {
     // no work: straight to the end
-  } else if (warp == 8 || warp == 9) {
+  } else if (warp == kLoadK || warp == kLoadV) {
     // ------------------------------ loads ------------------------------------------------------
-    const bool is_k = warp == 8;
+    const bool is_k = warp == kLoadK;
     const CUtensorMap* map = is_k ? &map_k : &map_v;
     const uint32_t full = sb + (is_k ? C::kKFull : C::kVFull), empty = sb + (is_k ? C::kKEmpty : C::kVEmpty);
     const uint32_t dst0 = sb + (is_k ? C::kOffK : C::kOffV);
@@ -228,7 +232,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
         while (!mbar_try_wait_brief(sb + C::kQFull, (n_piece - 1) & 1) && globaltimer_ns() - t0 < kWaitLimitNs) {}
       }
     }
-  } else if (warp == 10) {
+  } else if (warp == kIssue) {
     // ------------------------------ products: one thread ---------------------------------------
     if (elect_one()) {
       constexpr uint32_t idesc_s = umma_idesc_bf16(kSide, BK, false, false);  // S = Q K^T, both K-major
@@ -242,53 +246,81 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
         if (!mbar_wait_paced(bar, parity, abort_flag, p.status, kStatusCache | code)) ok = false;
         return ok;
       };
-      auto issue_s = [&](int side, uint32_t st) {
+      auto issue_s = [&](int side, int q_side, uint32_t st) {
 #pragma unroll
         for (int k = 0; k < DH / 16; ++k)
-          umma_ss(tmem + side * 128, dq + side * (C::kTileBytes >> 4) + (k / 4) * (C::kBoxBytes >> 4) + 2 * (k % 4),
+          umma_ss(tmem + side * 128, dq + q_side * (C::kTileBytes >> 4) + (k / 4) * (C::kBoxBytes >> 4) + 2 * (k % 4),
                   dk + st * (C::kTileBytes >> 4) + (k / 4) * (C::kBoxBytes >> 4) + 2 * (k % 4), idesc_s, k != 0 ? 1u : 0u);
         umma_commit(sb + C::kSFull + 8 * side);
       };
-      auto issue_pv = [&](int side, uint32_t st, bool first) {
+      auto issue_pv = [&](int side, uint32_t st, bool first) {  // 16 keys of P: 8 columns, in their half of the row's S
 #pragma unroll
         for (int k = 0; k < BK / 16; ++k)
-          umma_ts(tmem + C::kColO + side * DH, tmem + side * 128 + k * 8, dv + st * (C::kTileBytes >> 4) + k * (16 * 128 / 16), idesc_o,
-                  first && k == 0 ? 0u : 1u);
+          umma_ts(tmem + C::kColO + side * DH, tmem + side * 128 + (k / 4) * 64 + (k % 4) * 8,
+                  dv + st * (C::kTileBytes >> 4) + k * (16 * 128 / 16), idesc_o, first && k == 0 ? 0u : 1u);
       };
+      auto wait_k = [&]() { return wait(sb + C::kKFull + 8 * (kt % kStages), (kt / kStages) & 1, 6); };
+      auto wait_v = [&]() { return wait(sb + C::kVFull + 8 * (vt % kStages), (vt / kStages) & 1, 8); };
+      auto wait_p = [&](int side) {
+        if (!wait(sb + C::kPFull + 8 * side, cnt_p[side] & 1, 7)) return false;
+        ++cnt_p[side];
+        return true;
+      };
+      auto k_done = [&]() { umma_commit(sb + C::kKEmpty + 8 * (kt++ % kStages)); };
+      auto v_done = [&]() { umma_commit(sb + C::kVEmpty + 8 * (vt++ % kStages)); };
       for (; ok && walk.more(); walk.next(p, view)) {
         const AttnEntry e = view.entry[walk.entry];
         if (e.blocks == 0) continue;
         const int32_t n = walk.blocks();
-        const int sides = e.count > per_side ? 2 : 1;
         if (!wait(sb + C::kQFull, n_piece & 1, 5)) break;
         ++n_piece;
-        if (!wait(sb + C::kKFull + 8 * (kt % kStages), (kt / kStages) & 1, 6)) break;
-        tc_fence_after_sync();
-        for (int s = 0; s < sides; ++s) issue_s(s, kt % kStages);
-        umma_commit(sb + C::kKEmpty + 8 * (kt % kStages));
-        ++kt;
-        if (n == 1) umma_commit(sb + C::kQEmpty);
-        for (int32_t b = 0; b < n && ok; ++b) {
-          const uint32_t vs = vt % kStages;
-          for (int s = 0; s < sides; ++s) {
-            if (!wait(sb + C::kPFull + 8 * s, cnt_p[s] & 1, 7)) break;
-            ++cnt_p[s];
-            if (s == 0) {
-              if (!wait(sb + C::kVFull + 8 * vs, (vt / kStages) & 1, 8)) break;
-              if (b + 1 < n && !wait(sb + C::kKFull + 8 * (kt % kStages), (kt / kStages) & 1, 6)) break;
+        if (e.count > per_side) {  // two sides, every block for both
+          if (!wait_k()) break;
+          tc_fence_after_sync();
+          issue_s(0, 0, kt % kStages);
+          issue_s(1, 1, kt % kStages);
+          k_done();
+          if (n == 1) umma_commit(sb + C::kQEmpty);
+          for (int32_t i = 0; i < n && ok; ++i) {
+            for (int s = 0; s < 2; ++s) {
+              if (!wait_p(s)) break;
+              if (s == 0 && (!wait_v() || (i + 1 < n && !wait_k()))) break;
+              tc_fence_after_sync();
+              issue_pv(s, vt % kStages, i == 0);
+              if (i + 1 < n) issue_s(s, s, kt % kStages);
+              else umma_commit(sb + C::kOFull + 8 * s);
             }
+            if (!ok) break;
+            v_done();
+            if (i + 1 < n) {
+              k_done();
+              if (i + 2 == n) umma_commit(sb + C::kQEmpty);  // the piece's last S
+            }
+          }
+        } else {  // the same rows on both sides, every other block each
+          for (int s = 0; s < 2 && s < n; ++s) {
+            if (!wait_k()) break;
             tc_fence_after_sync();
-            issue_pv(s, vs, b == 0);
-            if (b + 1 < n) issue_s(s, kt % kStages);
-            else umma_commit(sb + C::kOFull + 8 * s);
+            issue_s(s, 0, kt % kStages);
+            k_done();
           }
           if (!ok) break;
-          umma_commit(sb + C::kVEmpty + 8 * vs);
-          ++vt;
-          if (b + 1 < n) {
-            umma_commit(sb + C::kKEmpty + 8 * (kt % kStages));
-            ++kt;
-            if (b + 2 == n) umma_commit(sb + C::kQEmpty);  // the piece's last S
+          if (n <= 2) umma_commit(sb + C::kQEmpty);
+          for (int32_t i = 0; i < n; ++i) {
+            const int s = i & 1;
+            if (!wait_p(s) || !wait_v()) break;
+            tc_fence_after_sync();
+            issue_pv(s, vt % kStages, i < 2);
+            v_done();
+            if (i + 2 < n) {
+              if (!wait_k()) break;
+              tc_fence_after_sync();
+              issue_s(s, 0, kt % kStages);
+              k_done();
+              if (i + 3 == n) umma_commit(sb + C::kQEmpty);
+            } else {
+              umma_commit(sb + C::kOFull + 8 * s);
+            }
           }
         }
       }
@@ -298,18 +330,33 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
         while (!mbar_try_wait_brief(sb + C::kDrain, 0) && globaltimer_ns() - t0 < kWaitLimitNs) {}
       }
     }
-  } else if (warp < 8) {
+  } else if (warp < kSoftmaxWarps) {
     // ------------------------------ softmax ----------------------------------------------------
-    const int side = warp / 4;
-    const int row = (warp % 4) * 32 + lane;  // of the side
-    const uint32_t t_lane = tmem + ((uint32_t)((warp % 4) * 32) << 16);
-    const uint32_t t_s = t_lane + side * 128, t_o = t_lane + C::kColO + side * DH;
-    uint32_t cnt_s = 0, cnt_o = 0;
+    const int side = warp / 8, half = (warp / 4) & 1, quad = warp % 4;
+    const int row = quad * 32 + lane;  // of the side
+    const uint32_t t_lane = tmem + ((uint32_t)(quad * 32) << 16);
+    const uint32_t t_s = t_lane + side * 128 + half * 64;  // this thread's columns of S; P goes to the first 32 of them
+    const uint32_t t_o = t_lane + C::kColO + side * DH + half * (DH / 2);
+    float* sum_own = reinterpret_cast<float*>(smem + C::kOffSum) + (side * 2 + half) * kSide + row;  // + 4 * 128 for odd blocks
+    const float* sum_other = reinterpret_cast<const float*>(smem + C::kOffSum) + (side * 2 + (half ^ 1)) * kSide + row;
+    float* max_own = reinterpret_cast<float*>(smem + C::kOffMax) + (side * 2 + half) * kSide + row;
+    const float* max_other = reinterpret_cast<const float*>(smem + C::kOffMax) + (side * 2 + (half ^ 1)) * kSide + row;
+    float4* ends = reinterpret_cast<float4*>(smem + C::kOffEnd) + row;  // + (side * 2 + half) * 128
+    uint32_t cnt_s = 0, cnt_o[2] = {0, 0}, cnt_pair = 0, cnt_quad = 0;
+    auto meet = [&](bool four) {  // the warps that share these 32 rows
+      __syncwarp();
+      const uint32_t bar = four ? sb + C::kQuad + 8 * quad : sb + C::kPair + 8 * (side * 4 + quad);
+      if (lane == 0) mbar_arrive(bar);
+      const bool met = mbar_wait_paced(bar, (four ? cnt_quad : cnt_pair) & 1, abort_flag, p.status, kStatusCache | 12);
+      if (four) ++cnt_quad; else ++cnt_pair;
+      return __all_sync(0xffffffffu, met) != 0;
+    };
     const int32_t side_rows = per_side * p.group;
     for (; walk.more(); walk.next(p, view)) {
       const AttnEntry e = view.entry[walk.entry];
-      if (side == 1 && e.count <= per_side) continue;
-      const int32_t t = side * per_side + row / p.group, h = walk.head * p.group + row % p.group;
+      const bool split = e.count <= per_side;  // both sides on the same rows
+      const int32_t tile_row = (split ? 0 : side * side_rows) + row;
+      const int32_t t = (split ? 0 : side * per_side) + row / p.group, h = walk.head * p.group + row % p.group;
       const bool there = row < side_rows && t < e.count;
       RowKeys keys{0, 0, 0};
       float slope = 0.f;
@@ -320,7 +367,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       const bool sees = there && keys.lo < keys.hi;
       uint8_t* out = p.O + (int64_t)(e.row0 + t) * p.o_row_bytes + h * p.o_head_bytes;
       if (e.blocks == 0) {  // nobody sees a key
-        if (there)
+        if (there && half == 0 && (!split || side == 0))
 #pragma unroll
           for (int c = 0; c < DH / 8; ++c) reinterpret_cast<uint4*>(out)[c] = make_uint4(0u, 0u, 0u, 0u);
         continue;
@@ -329,22 +376,26 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       const int32_t lo_most = __reduce_max_sync(0xffffffffu, there ? keys.lo : 0);
       const int32_t hi_least = __reduce_min_sync(0xffffffffu, there ? keys.hi : 0x7fffffff);
       const int32_t blk0 = e.blk0 + walk.block0(), n = walk.blocks();
+      const int32_t step = split ? 2 : 1, first = split ? side : 0;
       float m = sees ? -INFINITY : 0.f, l = 0.f;  // -inf: no reference yet
+      float last_sum = 0.f;
       bool aborted = false;
-      for (int32_t b = n - 1; b >= 0; --b) {
+      for (int32_t i = first; i < n; i += step) {
         if (!mbar_wait_paced(sb + C::kSFull + 8 * side, cnt_s & 1, abort_flag, p.status, kStatusCache | 10)) { aborted = true; break; }
         ++cnt_s;
         tc_fence_after_sync();
-        const int32_t j0 = (blk0 + b) * BK;
-        const bool full = j0 >= lo_most && j0 + BK <= hi_least;
-        // scores of columns c0.. of the row in log2 units but for the plain scale, -inf where the row does not see the key
+        const int32_t j0 = (blk0 + n - 1 - i) * BK + half * 64;  // the first of this thread's keys
+        const int32_t b0 = j0 - half * 64;
+        const bool full = b0 >= lo_most && b0 + BK <= hi_least;
+        // scores of columns c0.. in log2 units but for the plain scale, -inf where the row does not see the key
         auto scores = [&](int c0, uint32_t (&s)[32]) {
           if (CAP || BIAS) {
+            const float away = (float)(keys.pos - j0 - c0);
 #pragma unroll
             for (int x = 0; x < 32; ++x) {
               float v = __uint_as_float(s[x]) * p.scale;
               if (CAP) v = p.cap * tanh_fast(v);
-              if (BIAS) v = fmaf(-slope, fabsf((float)(keys.pos - j0 - c0 - x)), v);
+              if (BIAS) v = fmaf(-slope, fabsf(away - (float)x), v);
               s[x] = __float_as_uint(v);
             }
           }
@@ -356,114 +407,175 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
           }
         };
         const float scale = CAP || BIAS ? 1.f : p.scale;
-        bool slow = __any_sync(0xffffffffu, m == -INFINITY), moves = m == -INFINITY;
-        uint32_t pk[64];
-        float sum;
-        while (true) {
-          if (slow) {
-            float mx = -INFINITY;
-#pragma unroll 1
-            for (int c = 0; c < BK; c += 32) {
-              uint32_t s[32];
-              tmem_ld_32x32b_x32(t_s + c, s);
-              tmem_ld_wait();
-              scores(c, s);
-#pragma unroll
-              for (int x = 0; x < 32; ++x) mx = fmaxf(mx, __uint_as_float(s[x]));
-            }
-            mx *= scale;
-            const float m_new = moves ? fmaxf(m, mx) : m;
-            const float a = m_new == m ? 1.f : ex2_approx(m - m_new);
-            m = m_new;
-            l *= a;
-            if (b != n - 1 && __any_sync(0xffffffffu, a != 1.f)) {
-#pragma unroll 1
-              for (int c = 0; c < DH; c += 32) {
-                uint32_t o[32];
-                tmem_ld_32x32b_x32(t_o + c, o);
-                tmem_ld_wait();
-#pragma unroll
-                for (int x = 0; x < 32; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * a);
-                tmem_st_x32(t_o + c, o);
-              }
-              tmem_st_wait();
-            }
+        float a = 1.f;  // what O and the sum are scaled by
+        if (i != first) {
+          const float most = fmaxf(last_sum, sum_other[((cnt_s ^ 1) & 1) * 4 * kSide]);
+          if (most > kMoveAt) {
+            const int32_t up = (int32_t)(__float_as_uint(most) >> 23) - 127;
+            m += (float)up;
+            a = __uint_as_float((uint32_t)max(127 - up, 1) << 23);
           }
-          const float ref = m == -INFINITY ? 0.f : m;
-          const uint64_t c2 = pack2(scale, scale), m2 = pack2(-ref, -ref);
-          uint64_t sum2[2] = {pack2(0.f, 0.f), pack2(0.f, 0.f)};
-#pragma unroll
-          for (int c = 0; c < BK; c += 32) {
+        }
+        if (__any_sync(0xffffffffu, m == -INFINITY)) {  // rows without a reference: the maximum of this block
+          float mx = -INFINITY;
+#pragma unroll 1
+          for (int c = 0; c < 64; c += 32) {
             uint32_t s[32];
             tmem_ld_32x32b_x32(t_s + c, s);
             tmem_ld_wait();
             scores(c, s);
 #pragma unroll
-            for (int x = 0; x < 32; x += 2) {
-              float x0, x1;
-              unpack2(ffma2(pack2(__uint_as_float(s[x]), __uint_as_float(s[x + 1])), c2, m2), x0, x1);
-              const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
-              sum2[(x / 2) % 2] = fadd2(sum2[(x / 2) % 2], pack2(p0, p1));
-              pk[(c + x) / 2] = bf16_pair(p0, p1);
-            }
+            for (int x = 0; x < 32; ++x) mx = fmaxf(mx, __uint_as_float(s[x]));
           }
-          float s0, s1;
-          unpack2(fadd2(sum2[0], sum2[1]), s0, s1);
-          sum = s0 + s1;
-          moves = sees && !(sum <= kMoveAt);
-          if (slow || !__any_sync(0xffffffffu, moves)) break;
-          slow = true;
+          *max_own = mx * scale;
+          if (!meet(false)) { aborted = true; break; }
+          if (m == -INFINITY) m = fmaxf(mx * scale, *max_other);
         }
-        l += sum;
-        tmem_st_x32(t_s, pk);
-        tmem_st_x32(t_s + 32, pk + 32);
+        if (__any_sync(0xffffffffu, a != 1.f)) {
+          l *= a;
+#pragma unroll 1
+          for (int c = 0; c < DH / 2; c += 16) {
+            uint32_t o[16];
+            tmem_ld_32x32b_x16(t_o + c, o);
+            tmem_ld_wait();
+#pragma unroll
+            for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * a);
+            tmem_st_32x32b_x16(t_o + c, o);
+          }
+        }
+        const float ref = m == -INFINITY ? 0.f : m;
+        const uint64_t c2 = pack2(scale, scale), m2 = pack2(-ref, -ref);
+        uint64_t sum2 = pack2(0.f, 0.f);
+        uint32_t s[2][32];
+        tmem_ld_32x32b_x32(t_s, s[0]);
+        tmem_ld_wait();
+        tmem_ld_32x32b_x32(t_s + 32, s[1]);
+#pragma unroll
+        for (int c = 0; c < 2; ++c) {
+          if (c == 1) tmem_ld_wait();
+          scores(c * 32, s[c]);
+          uint32_t pk[16];
+#pragma unroll
+          for (int x = 0; x < 32; x += 2) {
+            float x0, x1;
+            unpack2(ffma2(pack2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])), c2, m2), x0, x1);
+            const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+            sum2 = fadd2(sum2, pack2(p0, p1));
+            pk[x / 2] = bf16_pair(p0, p1);
+          }
+          tmem_st_32x32b_x16(t_s + c * 16, pk);
+        }
+        float s0, s1;
+        unpack2(sum2, s0, s1);
+        last_sum = sees ? s0 + s1 : 0.f;
+        l += s0 + s1;
+        sum_own[(cnt_s & 1) * 4 * kSide] = last_sum;
         tmem_st_wait();
         tc_fence_before_sync();
         __syncwarp();
         if (lane == 0) mbar_arrive(sb + C::kPFull + 8 * side);
       }
       if (aborted) break;
-      if (!mbar_wait_paced(sb + C::kOFull + 8 * side, cnt_o & 1, abort_flag, p.status, kStatusCache | 11)) break;
-      ++cnt_o;
-      tc_fence_after_sync();
-      const bool whole = walk.whole();
-      const int32_t part = walk.part(), tile_row = side * side_rows + row;
-      const float inv = sees ? 1.f / l : 0.f;
-      float probe = l * 0.f;
-      float* to = attn_part(p, part) + (int64_t)tile_row * DH;
+      // ---- end of the piece: two (split: four) threads per row have a share of its columns each
+      const bool both = split && n > 1;  // O of either side
+      // Which sides' O this tile has, and which of them this thread reads.  (The arrivals of a side that it does not read are
+      // counted too: side A's of a piece comes in front of side B's, and both in front of the next piece's.)
+      bool done = true;
 #pragma unroll
-      for (int c = 0; c < DH; c += 32) {
-        uint32_t o[32];
-        tmem_ld_32x32b_x32(t_o + c, o);
+      for (int s = 0; s < 2; ++s) {
+        if (s == 1 && split && !both) continue;
+        if (split || s == side)
+          done = done && mbar_wait_paced(sb + C::kOFull + 8 * s, cnt_o[s] & 1, abort_flag, p.status, kStatusCache | 11);
+        ++cnt_o[s];
+      }
+      if (!done) break;
+      tc_fence_after_sync();
+      const int32_t width = split ? DH / 4 : DH / 2, col0 = (split ? side * 2 + half : half) * width;
+      const uint32_t t_a = t_lane + C::kColO + (split ? 0 : side * DH) + col0, t_b = t_lane + C::kColO + DH + col0;
+      float probe = 0.f;
+#pragma unroll 1
+      for (int c = 0; c < width; c += 16) {
+        uint32_t o[16];
+        tmem_ld_32x32b_x16(t_a + c, o);
         tmem_ld_wait();
 #pragma unroll
-        for (int x = 0; x < 32; ++x) probe = fmaf(__uint_as_float(o[x]), 0.f, probe);
-        if (!there) continue;
+        for (int x = 0; x < 16; ++x) probe = fmaf(__uint_as_float(o[x]), 0.f, probe);
+        if (both) {
+          tmem_ld_32x32b_x16(t_b + c, o);
+          tmem_ld_wait();
+#pragma unroll
+          for (int x = 0; x < 16; ++x) probe = fmaf(__uint_as_float(o[x]), 0.f, probe);
+        }
+      }
+      ends[(side * 2 + half) * kSide] = make_float4(m, l, probe, 0.f);
+      if (!meet(split)) break;
+      float wa = 1.f, wb = 0.f, m_all = m, l_all;
+      bool bad;
+      if (split) {
+        const float4 a0 = ends[0], a1 = ends[kSide], b0 = ends[2 * kSide], b1 = ends[3 * kSide];
+        bad = (a0.y + a1.y + b0.y + b1.y) * 0.f + a0.z + a1.z + b0.z + b1.z != 0.f;
+        m_all = a0.x;
+        l_all = a0.y + a1.y;
+        if (both) {
+          m_all = fmaxf(a0.x, b0.x);
+          const float r = m_all == -INFINITY ? 0.f : m_all;
+          wa = ex2_approx(a0.x - r);
+          wb = ex2_approx(b0.x - r);
+          l_all = wa * (a0.y + a1.y) + wb * (b0.y + b1.y);
+        }
+      } else {
+        const float4 a0 = ends[side * 2 * kSide], a1 = ends[(side * 2 + 1) * kSide];
+        bad = (a0.y + a1.y) * 0.f + a0.z + a1.z != 0.f;
+        l_all = a0.y + a1.y;
+      }
+      const bool whole = walk.whole();
+      const int32_t part = walk.part();
+      const float inv = whole ? (sees ? 1.f / l_all : 0.f) : 1.f;
+      wa *= inv;
+      wb *= inv;
+      const bool writes = there && !bad;
+      float* to = attn_part(p, part) + (int64_t)tile_row * DH + col0;
+#pragma unroll 1
+      for (int c = 0; c < width; c += 16) {
+        uint32_t o[16];
+        tmem_ld_32x32b_x16(t_a + c, o);
+        tmem_ld_wait();
+#pragma unroll
+        for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * wa);
+        if (both) {
+          uint32_t ob[16];
+          tmem_ld_32x32b_x16(t_b + c, ob);
+          tmem_ld_wait();
+#pragma unroll
+          for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(fmaf(__uint_as_float(ob[x]), wb, __uint_as_float(o[x])));
+        }
+        if (!writes) continue;
         if (whole) {
 #pragma unroll
-          for (int x = 0; x < 32; x += 8) {
+          for (int x = 0; x < 16; x += 8) {
             uint4 w;
-            w.x = bf16_pair(__uint_as_float(o[x]) * inv, __uint_as_float(o[x + 1]) * inv);
-            w.y = bf16_pair(__uint_as_float(o[x + 2]) * inv, __uint_as_float(o[x + 3]) * inv);
-            w.z = bf16_pair(__uint_as_float(o[x + 4]) * inv, __uint_as_float(o[x + 5]) * inv);
-            w.w = bf16_pair(__uint_as_float(o[x + 6]) * inv, __uint_as_float(o[x + 7]) * inv);
-            *reinterpret_cast<uint4*>(out + (c + x) * 2) = w;
+            w.x = bf16_pair(__uint_as_float(o[x]), __uint_as_float(o[x + 1]));
+            w.y = bf16_pair(__uint_as_float(o[x + 2]), __uint_as_float(o[x + 3]));
+            w.z = bf16_pair(__uint_as_float(o[x + 4]), __uint_as_float(o[x + 5]));
+            w.w = bf16_pair(__uint_as_float(o[x + 6]), __uint_as_float(o[x + 7]));
+            *reinterpret_cast<uint4*>(out + (col0 + c + x) * 2) = w;
           }
         } else {
 #pragma unroll
-          for (int x = 0; x < 32; x += 4)
+          for (int x = 0; x < 16; x += 4)
             *reinterpret_cast<float4*>(to + c + x) = make_float4(__uint_as_float(o[x]), __uint_as_float(o[x + 1]), __uint_as_float(o[x + 2]),
                                                                  __uint_as_float(o[x + 3]));
         }
       }
-      if (there && !whole) attn_part_sums(p, gridDim.x, part)[tile_row] = make_float2(m, l);
+      const bool leads = half == 0 && (!split || side == 0);  // of the threads of a row
+      if (writes && !whole && leads) attn_part_sums(p, gridDim.x, part)[tile_row] = make_float2(m_all, l_all);
       tc_fence_before_sync();  // the next piece's first P V overwrites O
-      uint32_t bad = __ballot_sync(0xffffffffu, there && probe != 0.f);
-      __syncwarp();
-      while (bad != 0) {  // a row at a time, by the warp
-        const int src = __ffs(bad) - 1;
-        bad &= bad - 1;
-        const int32_t r = (warp % 4) * 32 + src, rt = side * per_side + r / p.group, rh = walk.head * p.group + r % p.group;
+      if (split && !meet(true)) break;  // the other side has read this one's O
+      uint32_t redo = __ballot_sync(0xffffffffu, there && bad && leads);
+      while (redo != 0) {  // a row at a time, by the warp
+        const int src = __ffs(redo) - 1;
+        redo &= redo - 1;
+        const int32_t r = quad * 32 + src, rt = (split ? 0 : side * per_side) + r / p.group, rh = walk.head * p.group + r % p.group;
         const RowKeys rk = attn_row(p, e, rt);
         float acc[DH / 32], mm, ll;
         attn_row_by_hand<DH>(p, e, (int64_t)(walk.head / p.per_kv) * p.head_bytes,
@@ -474,10 +586,11 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
 #pragma unroll
           for (int c = 0; c < DH / 32; ++c) o[lane + 32 * c] = __float2bfloat16_rn(rk.lo < rk.hi ? acc[c] / ll : 0.f);
         } else {
-          float* o = attn_part(p, part) + (int64_t)(side * side_rows + r) * DH;
+          const int32_t tr = (split ? 0 : side * side_rows) + r;
+          float* o = attn_part(p, part) + (int64_t)tr * DH;
 #pragma unroll
           for (int c = 0; c < DH / 32; ++c) o[lane + 32 * c] = acc[c];
-          if (lane == 0) attn_part_sums(p, gridDim.x, part)[side * side_rows + r] = make_float2(mm, ll);
+          if (lane == 0) attn_part_sums(p, gridDim.x, part)[tr] = make_float2(mm, ll);
         }
       }
     }
@@ -485,7 +598,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
 
   tc_fence_before_sync();
   __syncthreads();
-  if (warp == 10) {
+  if (warp == kIssue) {
     tc_fence_after_sync();
     tmem_dealloc(tmem, 512);
   }
