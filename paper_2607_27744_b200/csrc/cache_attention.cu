@@ -114,8 +114,8 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(CacheAttn p, int32_t
 }
 
 template <typename T>
-rocs_status_t join_parts(const CacheAttn& p, int32_t grid, cudaStream_t stream) {
-  const dim3 blocks((unsigned)grid, (unsigned)(p.tile_rows / 4));
+rocs_status_t join_parts(const CacheAttn& p, int32_t rows, int32_t grid, cudaStream_t stream) {
+  const dim3 blocks((unsigned)grid, (unsigned)std::min((rows + 3) / 4, 32));
   if (p.dh <= 64) return launch_dependent(join_kernel<T, 2>, blocks, kJoinThreads, 0, stream, p, grid);
   if (p.dh <= 128) return launch_dependent(join_kernel<T, 4>, blocks, kJoinThreads, 0, stream, p, grid);
   return launch_dependent(join_kernel<T, 8>, blocks, kJoinThreads, 0, stream, p, grid);
@@ -492,7 +492,8 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
                            : x.kind == Kind::kMma ? attn_mma(p, x.grid, stream)
                                                   : attn_general(c->dtype, p, x.grid, stream);
   if (st != ROCS_OK) return st;
-  return c->dtype == ROCS_BF16 ? join_parts<__nv_bfloat16>(p, x.grid, stream) : join_parts<float>(p, x.grid, stream);
+  const int32_t rows = (int32_t)std::min<int64_t>(x.tile_rows, (int64_t)plan->largest * x.group);  // most of a tile
+  return c->dtype == ROCS_BF16 ? join_parts<__nv_bfloat16>(p, rows, x.grid, stream) : join_parts<float>(p, rows, x.grid, stream);
 }
 
 }  // extern "C"

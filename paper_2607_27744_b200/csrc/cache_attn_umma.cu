@@ -22,6 +22,7 @@
 // A row whose scores pass its reference by more than fp32's range within one block, or whose masked keys hold NaN or Inf
 // values (weight 0, but 0 x Inf is not 0), comes out non-finite and is computed again from the keys that it sees, by a warp.
 #include <algorithm>
+#include <type_traits>
 
 #include "cache_attn.cuh"
 
@@ -35,6 +36,7 @@ constexpr int kUmmaThreads = 20 * 32;
 constexpr int kSide = 128;               // rows of a side = tensor memory lanes
 constexpr int BK = kUmmaKeys;
 constexpr uint32_t kStatusCache = 0x500;
+constexpr int kOnFma = 3;  // of eight pairs of exponentials
 constexpr float kMoveAt = 1099511627776.f;  // 2^40
 
 template <int DH_>
@@ -47,8 +49,8 @@ struct UmmaCfg {
   static constexpr uint32_t kOffQ = 0;
   static constexpr uint32_t kOffK = kOffQ + 2 * kTileBytes;
   static constexpr uint32_t kOffV = kOffK + kStages * kTileBytes;
-  static constexpr uint32_t kOffSum = kOffV + kStages * kTileBytes;   // [2 parities][2 sides][2 halves][128] sums of a block
-  static constexpr uint32_t kOffMax = kOffSum + 8 * kSide * 4;        // [2 sides][2 halves][128] maxima of a block
+  static constexpr uint32_t kOffSum = kOffV + kStages * kTileBytes;   // [4 blocks][2 sides][2 halves][128] sums of a block
+  static constexpr uint32_t kOffMax = kOffSum + 16 * kSide * 4;       // [2 sides][2 halves][128] maxima of a block
   static constexpr uint32_t kOffEnd = kOffMax + 4 * kSide * 4;        // [2 sides][2 halves][128] (reference, sum, probe, -)
   static constexpr uint32_t kOffBar = kOffEnd + 4 * kSide * 16;
   static constexpr uint32_t kQFull = kOffBar, kQEmpty = kQFull + 8, kSFull = kQEmpty + 8, kPFull = kSFull + 16, kOFull = kPFull + 16,
@@ -82,10 +84,34 @@ __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64
       "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+__device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t* r) {
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
+               "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
+               : "memory");
+}
 __device__ __forceinline__ uint64_t fadd2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
+}
+
+// 2^x for a pair on the FMA pipes: 2^n 2^f with n the nearest integer and a polynomial of degree 3 for 2^f on [-1/2, 1/2]
+// (fitted for the least relative error, 7.5e-5: a 26th of the rounding to bf16 that follows).  Below 2^-125 it stays there.
+__device__ __forceinline__ uint64_t exp2_pair(uint64_t x2) {
+  float x0, x1;
+  unpack2(x2, x0, x1);
+  const uint64_t x = pack2(fmaxf(x0, -125.f), fmaxf(x1, -125.f));
+  constexpr float kMagic = 12582912.f;  // 1.5 x 2^23: the sum's last bits are the nearest integer
+  const uint64_t t = fadd2(x, pack2(kMagic, kMagic));
+  const uint64_t f = fadd2(x, ffma2(t, pack2(-1.f, -1.f), pack2(kMagic, kMagic)));
+  uint64_t r = ffma2(f, pack2(0.0551716685295105f, 0.0551716685295105f), pack2(0.2426111251115799f, 0.2426111251115799f));
+  r = ffma2(r, f, pack2(0.6932609677314758f, 0.6932609677314758f));
+  r = ffma2(r, f, pack2(0.9999280571937561f, 0.9999280571937561f));
+  float t0, t1, r0, r1;
+  unpack2(t, t0, t1);
+  unpack2(r, r0, r1);
+  return pack2(__uint_as_float(__float_as_uint(r0) + (__float_as_uint(t0) << 23)),
+               __uint_as_float(__float_as_uint(r1) + (__float_as_uint(t1) << 23)));
 }
 
 template <int DH, bool CAP, bool BIAS>
@@ -283,8 +309,8 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
           if (n == 1) umma_commit(sb + C::kQEmpty);
           for (int32_t i = 0; i < n && ok; ++i) {
             for (int s = 0; s < 2; ++s) {
+              if (s == 0 && (!wait_v() || (i + 1 < n && !wait_k()))) break;  // long there, as a rule: not behind the wait for P
               if (!wait_p(s)) break;
-              if (s == 0 && (!wait_v() || (i + 1 < n && !wait_k()))) break;
               tc_fence_after_sync();
               issue_pv(s, vt % kStages, i == 0);
               if (i + 1 < n) issue_s(s, s, kt % kStages);
@@ -308,13 +334,11 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
           if (n <= 2) umma_commit(sb + C::kQEmpty);
           for (int32_t i = 0; i < n; ++i) {
             const int s = i & 1;
-            if (!wait_p(s) || !wait_v()) break;
+            if (!wait_v() || (i + 2 < n && !wait_k()) || !wait_p(s)) break;
             tc_fence_after_sync();
             issue_pv(s, vt % kStages, i < 2);
             v_done();
             if (i + 2 < n) {
-              if (!wait_k()) break;
-              tc_fence_after_sync();
               issue_s(s, 0, kt % kStages);
               k_done();
               if (i + 3 == n) umma_commit(sb + C::kQEmpty);
@@ -378,98 +402,132 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       const int32_t blk0 = e.blk0 + walk.block0(), n = walk.blocks();
       const int32_t step = split ? 2 : 1, first = split ? side : 0;
       float m = sees ? -INFINITY : 0.f, l = 0.f;  // -inf: no reference yet
-      float last_sum = 0.f;
+      float own[2] = {0.f, 0.f};  // this half's sums of the last two blocks
+      float moved = 1.f;          // 2^(what the reference moved by for the last block)
       bool aborted = false;
       for (int32_t i = first; i < n; i += step) {
+        // The reference moves by what the block before the last one summed to: that the other half's sum of it is there is
+        // known since the last block's S arrived, so that nothing of this comes behind this block's.
+        float up = 0.f;
+        if (i >= first + 2 * step) {
+          const float most = fmaxf(own[cnt_s & 1], sum_other[((cnt_s - 2) & 3) * 4 * kSide]);
+          // (as long as the reference moved for the block in front of it, its sum was that of the old one)
+          if (most > kMoveAt * moved) up = (float)((int32_t)(__float_as_uint(most / moved) >> 23) - 127);
+        }
+        const bool slow = __any_sync(0xffffffffu, m == -INFINITY || up != 0.f);
         if (!mbar_wait_paced(sb + C::kSFull + 8 * side, cnt_s & 1, abort_flag, p.status, kStatusCache | 10)) { aborted = true; break; }
-        ++cnt_s;
         tc_fence_after_sync();
-        const int32_t j0 = (blk0 + n - 1 - i) * BK + half * 64;  // the first of this thread's keys
-        const int32_t b0 = j0 - half * 64;
-        const bool full = b0 >= lo_most && b0 + BK <= hi_least;
+        const int32_t b0 = (blk0 + n - 1 - i) * BK, j0 = b0 + half * 64;  // the block's first key, this thread's
+        const bool all_begun = b0 >= lo_most, none_ended = b0 + BK <= hi_least;  // what masks may be left out
         // scores of columns c0.. in log2 units but for the plain scale, -inf where the row does not see the key
-        auto scores = [&](int c0, uint32_t (&s)[32]) {
+        auto scores = [&](int c0, uint32_t (&s)[16]) {
           if (CAP || BIAS) {
             const float away = (float)(keys.pos - j0 - c0);
 #pragma unroll
-            for (int x = 0; x < 32; ++x) {
+            for (int x = 0; x < 16; ++x) {
               float v = __uint_as_float(s[x]) * p.scale;
               if (CAP) v = p.cap * tanh_fast(v);
               if (BIAS) v = fmaf(-slope, fabsf(away - (float)x), v);
               s[x] = __float_as_uint(v);
             }
           }
-          if (!full) {
-            const int32_t lo = keys.lo - j0 - c0, hi = keys.hi - j0 - c0;
+          if (!all_begun) {
+            const int32_t lo = keys.lo - j0 - c0;
 #pragma unroll
-            for (int x = 0; x < 32; ++x)
-              if (x < lo || x >= hi) s[x] = 0xff800000u;
+            for (int x = 0; x < 16; ++x)
+              if (x < lo) s[x] = 0xff800000u;
+          }
+          if (!none_ended) {
+            const int32_t hi = keys.hi - j0 - c0;
+#pragma unroll
+            for (int x = 0; x < 16; ++x)
+              if (x >= hi) s[x] = 0xff800000u;
           }
         };
         const float scale = CAP || BIAS ? 1.f : p.scale;
-        float a = 1.f;  // what O and the sum are scaled by
-        if (i != first) {
-          const float most = fmaxf(last_sum, sum_other[((cnt_s ^ 1) & 1) * 4 * kSide]);
-          if (most > kMoveAt) {
-            const int32_t up = (int32_t)(__float_as_uint(most) >> 23) - 127;
-            m += (float)up;
-            a = __uint_as_float((uint32_t)max(127 - up, 1) << 23);
-          }
-        }
-        if (__any_sync(0xffffffffu, m == -INFINITY)) {  // rows without a reference: the maximum of this block
-          float mx = -INFINITY;
+        if (slow) {
+          if (__any_sync(0xffffffffu, m == -INFINITY)) {  // rows without a reference: the maximum of this block
+            float mx = -INFINITY;
 #pragma unroll 1
-          for (int c = 0; c < 64; c += 32) {
-            uint32_t s[32];
-            tmem_ld_32x32b_x32(t_s + c, s);
-            tmem_ld_wait();
-            scores(c, s);
+            for (int c = 0; c < 64; c += 16) {
+              uint32_t s[16];
+              tmem_ld_32x32b_x16(t_s + c, s);
+              tmem_ld_wait();
+              scores(c, s);
 #pragma unroll
-            for (int x = 0; x < 32; ++x) mx = fmaxf(mx, __uint_as_float(s[x]));
+              for (int x = 0; x < 16; ++x) mx = fmaxf(mx, __uint_as_float(s[x]));
+            }
+            *max_own = mx * scale;
+            if (!meet(false)) { aborted = true; break; }
+            if (m == -INFINITY) m = fmaxf(mx * scale, *max_other);
           }
-          *max_own = mx * scale;
-          if (!meet(false)) { aborted = true; break; }
-          if (m == -INFINITY) m = fmaxf(mx * scale, *max_other);
-        }
-        if (__any_sync(0xffffffffu, a != 1.f)) {
-          l *= a;
+          if (__any_sync(0xffffffffu, up != 0.f)) {
+            const float a = __uint_as_float((uint32_t)max(127 - (int32_t)up, 0) << 23);  // 2^-up
+            m += up;
+            l *= a;
 #pragma unroll 1
-          for (int c = 0; c < DH / 2; c += 16) {
-            uint32_t o[16];
-            tmem_ld_32x32b_x16(t_o + c, o);
-            tmem_ld_wait();
+            for (int c = 0; c < DH / 2; c += 16) {
+              uint32_t o[16];
+              tmem_ld_32x32b_x16(t_o + c, o);
+              tmem_ld_wait();
 #pragma unroll
-            for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * a);
-            tmem_st_32x32b_x16(t_o + c, o);
+              for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * a);
+              tmem_st_32x32b_x16(t_o + c, o);
+            }
           }
         }
+        moved = __uint_as_float((uint32_t)min(127 + (int32_t)up, 254) << 23);
         const float ref = m == -INFINITY ? 0.f : m;
         const uint64_t c2 = pack2(scale, scale), m2 = pack2(-ref, -ref);
         uint64_t sum2 = pack2(0.f, 0.f);
-        uint32_t s[2][32];
-        tmem_ld_32x32b_x32(t_s, s[0]);
+        // 16 columns at a time, the next ones on their way (P's columns are those of scores that have been read)
+        uint32_t s[2][16];
+        tmem_ld_32x32b_x16(t_s, s[0]);
         tmem_ld_wait();
-        tmem_ld_32x32b_x32(t_s + 32, s[1]);
+        // `some`: how many of eight pairs take the FMA pipes instead of the special-function unit, whose 16 results a cycle
+        // would be what the kernel waits for
+        auto weights = [&](int c, auto some) {
+          uint32_t pk[8];
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          if (c == 1) tmem_ld_wait();
-          scores(c * 32, s[c]);
-          uint32_t pk[16];
-#pragma unroll
-          for (int x = 0; x < 32; x += 2) {
-            float x0, x1;
-            unpack2(ffma2(pack2(__uint_as_float(s[c][x]), __uint_as_float(s[c][x + 1])), c2, m2), x0, x1);
-            const float p0 = ex2_approx(x0), p1 = ex2_approx(x1);
+          for (int x = 0; x < 16; x += 2) {
+            const uint64_t x2 = ffma2(pack2(__uint_as_float(s[c % 2][x]), __uint_as_float(s[c % 2][x + 1])), c2, m2);
+            float p0, p1;
+            if ((x / 2 * 3) % 8 < decltype(some)::value) {
+              unpack2(exp2_pair(x2), p0, p1);
+            } else {
+              float x0, x1;
+              unpack2(x2, x0, x1);
+              p0 = ex2_approx(x0);
+              p1 = ex2_approx(x1);
+            }
             sum2 = fadd2(sum2, pack2(p0, p1));
             pk[x / 2] = bf16_pair(p0, p1);
           }
-          tmem_st_32x32b_x16(t_s + c * 16, pk);
+          tmem_st_x8(t_s + c * 8, pk);
+        };
+        if (all_begun && none_ended) {
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            if (c > 0) tmem_ld_wait();
+            if (c < 3) tmem_ld_32x32b_x16(t_s + (c + 1) * 16, s[(c + 1) % 2]);
+            scores(c * 16, s[c % 2]);
+            weights(c, std::integral_constant<int, kOnFma>());
+          }
+        } else {  // (a masked key's weight is 0 from the special-function unit, not 2^-125)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            if (c > 0) tmem_ld_wait();
+            if (c < 3) tmem_ld_32x32b_x16(t_s + (c + 1) * 16, s[(c + 1) % 2]);
+            scores(c * 16, s[c % 2]);
+            weights(c, std::integral_constant<int, 0>());
+          }
         }
         float s0, s1;
         unpack2(sum2, s0, s1);
-        last_sum = sees ? s0 + s1 : 0.f;
+        own[cnt_s & 1] = sees ? s0 + s1 : 0.f;
         l += s0 + s1;
-        sum_own[(cnt_s & 1) * 4 * kSide] = last_sum;
+        sum_own[(cnt_s & 3) * 4 * kSide] = own[cnt_s & 1];
+        ++cnt_s;
         tmem_st_wait();
         tc_fence_before_sync();
         __syncwarp();
@@ -492,28 +550,11 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       tc_fence_after_sync();
       const int32_t width = split ? DH / 4 : DH / 2, col0 = (split ? side * 2 + half : half) * width;
       const uint32_t t_a = t_lane + C::kColO + (split ? 0 : side * DH) + col0, t_b = t_lane + C::kColO + DH + col0;
-      float probe = 0.f;
-#pragma unroll 1
-      for (int c = 0; c < width; c += 16) {
-        uint32_t o[16];
-        tmem_ld_32x32b_x16(t_a + c, o);
-        tmem_ld_wait();
-#pragma unroll
-        for (int x = 0; x < 16; ++x) probe = fmaf(__uint_as_float(o[x]), 0.f, probe);
-        if (both) {
-          tmem_ld_32x32b_x16(t_b + c, o);
-          tmem_ld_wait();
-#pragma unroll
-          for (int x = 0; x < 16; ++x) probe = fmaf(__uint_as_float(o[x]), 0.f, probe);
-        }
-      }
-      ends[(side * 2 + half) * kSide] = make_float4(m, l, probe, 0.f);
+      ends[(side * 2 + half) * kSide] = make_float4(m, l, 0.f, 0.f);
       if (!meet(split)) break;
       float wa = 1.f, wb = 0.f, m_all = m, l_all;
-      bool bad;
       if (split) {
         const float4 a0 = ends[0], a1 = ends[kSide], b0 = ends[2 * kSide], b1 = ends[3 * kSide];
-        bad = (a0.y + a1.y + b0.y + b1.y) * 0.f + a0.z + a1.z + b0.z + b1.z != 0.f;
         m_all = a0.x;
         l_all = a0.y + a1.y;
         if (both) {
@@ -521,35 +562,35 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
           const float r = m_all == -INFINITY ? 0.f : m_all;
           wa = ex2_approx(a0.x - r);
           wb = ex2_approx(b0.x - r);
-          l_all = wa * (a0.y + a1.y) + wb * (b0.y + b1.y);
+          l_all = wa * l_all + wb * (b0.y + b1.y);
         }
       } else {
-        const float4 a0 = ends[side * 2 * kSide], a1 = ends[(side * 2 + 1) * kSide];
-        bad = (a0.y + a1.y) * 0.f + a0.z + a1.z != 0.f;
-        l_all = a0.y + a1.y;
+        l_all = ends[side * 2 * kSide].y + ends[(side * 2 + 1) * kSide].y;
       }
       const bool whole = walk.whole();
       const int32_t part = walk.part();
       const float inv = whole ? (sees ? 1.f / l_all : 0.f) : 1.f;
-      wa *= inv;
-      wb *= inv;
-      const bool writes = there && !bad;
+      // non-finite, or only scores of -inf, which exp2_pair does not take to 0: by hand
+      float probe = m == -INFINITY && l != 0.f ? NAN : l * 0.f;
       float* to = attn_part(p, part) + (int64_t)tile_row * DH + col0;
 #pragma unroll 1
       for (int c = 0; c < width; c += 16) {
-        uint32_t o[16];
+        uint32_t o[16], ob[16];
         tmem_ld_32x32b_x16(t_a + c, o);
+        if (both) tmem_ld_32x32b_x16(t_b + c, ob);
         tmem_ld_wait();
 #pragma unroll
-        for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(__uint_as_float(o[x]) * wa);
-        if (both) {
-          uint32_t ob[16];
-          tmem_ld_32x32b_x16(t_b + c, ob);
-          tmem_ld_wait();
-#pragma unroll
-          for (int x = 0; x < 16; ++x) o[x] = __float_as_uint(fmaf(__uint_as_float(ob[x]), wb, __uint_as_float(o[x])));
+        for (int x = 0; x < 16; ++x) {
+          float v = __uint_as_float(o[x]);
+          probe = fmaf(v, 0.f, probe);
+          v *= wa;
+          if (both) {
+            probe = fmaf(__uint_as_float(ob[x]), 0.f, probe);
+            v = fmaf(__uint_as_float(ob[x]), wb, v);
+          }
+          o[x] = __float_as_uint(v * inv);
         }
-        if (!writes) continue;
+        if (!there) continue;
         if (whole) {
 #pragma unroll
           for (int x = 0; x < 16; x += 8) {
@@ -568,10 +609,16 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
         }
       }
       const bool leads = half == 0 && (!split || side == 0);  // of the threads of a row
-      if (writes && !whole && leads) attn_part_sums(p, gridDim.x, part)[tile_row] = make_float2(m_all, l_all);
+      if (there && !whole && leads) attn_part_sums(p, gridDim.x, part)[tile_row] = make_float2(m_all, l_all);
+      ends[(side * 2 + half) * kSide].z = probe;
       tc_fence_before_sync();  // the next piece's first P V overwrites O
-      if (split && !meet(true)) break;  // the other side has read this one's O
-      uint32_t redo = __ballot_sync(0xffffffffu, there && bad && leads);
+      if (!meet(split)) break;  // O has been read, and what there is of a row written
+      bool bad = false;
+      if (leads) {
+        bad = there && (split ? ends[0].z + ends[kSide].z + ends[2 * kSide].z + ends[3 * kSide].z
+                              : ends[side * 2 * kSide].z + ends[(side * 2 + 1) * kSide].z) != 0.f;
+      }
+      uint32_t redo = __ballot_sync(0xffffffffu, bad);
       while (redo != 0) {  // a row at a time, by the warp
         const int src = __ffs(redo) - 1;
         redo &= redo - 1;
