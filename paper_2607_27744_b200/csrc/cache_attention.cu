@@ -143,7 +143,7 @@ __global__ void __launch_bounds__(kGenThreads) general_kernel(const CacheAttn p)
   ptx::griddep_launch_dependents();
   const AttnLineView view = attn_line<kGenThreads>(p, line_mem);
   AttnWalk walk;
-  if (!walk.start(p, view)) return;
+  if (!walk.start<kGenThreads - 1>(p, view)) return;
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const int32_t dh = p.dh, row_bytes = gen_row_bytes<T>(dh), vecs = dh * (int)sizeof(T) / 16;
   float* qs = reinterpret_cast<float*>(smem);

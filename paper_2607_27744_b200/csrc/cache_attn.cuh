@@ -75,6 +75,7 @@ inline bool make_page_map(CUtensorMap* map, const void* base, const CacheAttn& p
 struct AttnLine {
   int64_t line[kLocalEntries + 1];
   AttnEntry entry[kLocalEntries];
+  uint32_t sums[kLocalEntries / 32];
 };
 struct AttnLineView {
   const int64_t* line;
@@ -136,21 +137,25 @@ __device__ __forceinline__ AttnLineView attn_line(const CacheAttn& p, AttnLine& 
     mem.entry[i] = e;
   }
   __syncthreads();
-  if (threadIdx.x < 32) {
-    int64_t base = 0;
-    for (int32_t i0 = 0; i0 < p.entries; i0 += 32) {
-      const int32_t i = i0 + (int32_t)threadIdx.x;
-      const int64_t cost = i < p.entries ? attn_cost(mem.entry[i]) : 0;
-      int64_t incl = cost;
+  // (a tile's cost is below 2^26: 32 of them stay in 32 bits)
+  static_assert(kLocalEntries == 128 && THREADS >= 128, "four warps of entries");
+  uint32_t cost = 0, incl = 0;
+  if (threadIdx.x < kLocalEntries) {
+    cost = (int32_t)threadIdx.x < p.entries ? (uint32_t)attn_cost(mem.entry[threadIdx.x]) : 0u;
+    incl = cost;
 #pragma unroll
-      for (int o = 1; o < 32; o <<= 1) {
-        const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
-        if ((int)threadIdx.x >= o) incl += up;
-      }
-      if (i < p.entries) mem.line[i] = base + incl - cost;
-      base += __shfl_sync(0xffffffffu, incl, 31);
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t up = __shfl_up_sync(0xffffffffu, incl, o);
+      if ((int)(threadIdx.x % 32) >= o) incl += up;
     }
-    if (threadIdx.x == 0) mem.line[p.entries] = base;
+    if (threadIdx.x % 32 == 31) mem.sums[threadIdx.x / 32] = incl;
+  }
+  __syncthreads();
+  if (threadIdx.x < kLocalEntries) {
+    int64_t base = 0;
+    for (int w = 0; w < (int)threadIdx.x / 32; ++w) base += mem.sums[w];
+    if ((int32_t)threadIdx.x <= p.entries) mem.line[threadIdx.x] = base + (incl - cost);
+    if ((int)threadIdx.x == kLocalEntries - 1 && p.entries == kLocalEntries) mem.line[kLocalEntries] = base + incl;
   }
   __syncthreads();
   return AttnLineView{mem.line, mem.entry};
@@ -162,20 +167,28 @@ struct AttnWalk {
   int64_t tile_begin;  // unit at which the tile at hand begins
   int32_t entry, head, cost;
   bool first;          // the piece at hand is the CTA's first
-  __device__ __forceinline__ static int64_t cut(int64_t total, int32_t ctas, int32_t i) { return total * i / ctas; }
-  // false: nothing for this CTA.  Thread 0 notes what the joining kernel needs.
+  // x / d for d < 2^31; most lines are short enough for one instruction's worth of division
+  __device__ __forceinline__ static int64_t over(int64_t x, int32_t d) {
+    return x >> 32 == 0 ? (int64_t)((uint32_t)x / (uint32_t)d) : x / d;
+  }
+  // false: nothing for this CTA.  Its thread NOTER, one that has little else to do, notes what the joining kernel needs.
+  template <int NOTER>
   __device__ __forceinline__ bool start(const CacheAttn& p, const AttnLineView& v) {
     const int64_t total = v.line[p.entries] * p.heads;
-    const int32_t ctas = (int32_t)min((int64_t)gridDim.x, max(total / p.min_units, (int64_t)1));
+    const int32_t ctas = (int32_t)min((int64_t)gridDim.x, max(over(total, p.min_units), (int64_t)1));
     const int32_t i = blockIdx.x;
     u = end = 0;
     first = true;
     if (i >= ctas || total == 0) {
-      if (threadIdx.x == 0) p.meta[i].parts = 0;
+      if (threadIdx.x == NOTER) p.meta[i].parts = 0;
       return false;
     }
-    u = cut(total, ctas, i);
-    end = cut(total, ctas, i + 1);
+    // the first `more` CTAs have a unit more than the others
+    const int64_t each = over(total, ctas);
+    const int32_t more = (int32_t)(total - each * ctas);
+    auto cut = [&](int32_t x) { return each * x + min(x, more); };
+    u = cut(i);
+    end = cut(i + 1);
     int32_t lo = 0, hi = p.entries;  // largest entry that begins at or before u
     while (hi - lo > 1) {
       const int32_t mid = lo + (hi - lo) / 2;
@@ -184,18 +197,19 @@ struct AttnWalk {
     entry = lo;
     cost = (int32_t)(v.line[lo + 1] - v.line[lo]);
     const int64_t in = u - v.line[lo] * p.heads;
-    head = (int32_t)(in / cost);
+    head = (int32_t)over(in, cost);
     tile_begin = v.line[lo] * p.heads + (int64_t)head * cost;
-    if (threadIdx.x == 0) {
+    if (threadIdx.x == NOTER) {
       AttnMeta m;
       m.parts = 0;
       if (u > tile_begin) {
-        const int64_t in_front = cut(total, ctas, i - 1);
+        const int64_t in_front = cut(i - 1), last = tile_begin + cost - 1;
         if (in_front <= tile_begin) {
           m.entry = v.entry[entry];
           m.head = head;
-          m.parts = 1;
-          while (i - 1 + m.parts < ctas && cut(total, ctas, i - 1 + m.parts) < tile_begin + cost) ++m.parts;
+          const int64_t longer = (each + 1) * more;  // units of those CTAs; the one that has unit `last`:
+          const int32_t at = last < longer ? (int32_t)(last / (each + 1)) : more + (int32_t)((last - longer) / each);
+          m.parts = at - (i - 1) + 1;
           m.place = 2 * (i - 1) + (in_front == tile_begin ? 0 : 1);
         }
       }

@@ -114,7 +114,7 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
   const AttnLineView view = attn_line<kFewThreads>(p, line_mem);
   __syncthreads();
   AttnWalk walk;
-  if (!walk.start(p, view)) return;
+  if (!walk.start<127>(p, view)) return;
   if (warp == 4) {
     // ------------------------------ loads ------------------------------------------------------
     const int32_t box_rows = min(p.page, kFewKeys), boxes = kFewKeys / box_rows;  // pages (or parts of one) of a block

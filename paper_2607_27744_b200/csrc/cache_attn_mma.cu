@@ -66,7 +66,7 @@ __global__ void __launch_bounds__(kMmaThreads, MmaCfg<DH>::kPerSm) mma_kernel(co
   ptx::griddep_launch_dependents();
   const AttnLineView view = attn_line<kMmaThreads>(p, line_mem);
   AttnWalk walk;
-  if (!walk.start(p, view)) return;
+  if (!walk.start<kMmaThreads - 1>(p, view)) return;
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   const uint32_t sb = ptx::smem_u32(smem);
   float* merge = reinterpret_cast<float*>(smem + C::kStages * C::kStageBytes);

@@ -166,7 +166,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
   griddep_launch_dependents();
   const AttnLineView view = attn_line<kUmmaThreads>(p, line_mem);
   AttnWalk walk;
-  const bool any = walk.start(p, view);
+  const bool any = walk.start<kUmmaThreads - 1>(p, view);
   const int32_t per_side = p.rows_per_tile / 2;  // batch rows of a side
 
   if (!any) {
