@@ -11,47 +11,54 @@ namespace {
 constexpr int kLineThreads = 1024;
 constexpr float kLog2e = 1.4426950408889634f;
 
-// The line of a launch with more tiles than a CTA's shared memory keeps, or whose rows begin somewhere (their first key
-// takes a look at every row: a warp per entry).
+// The tiles of a launch that has more of them than a CTA's shared memory keeps, or whose rows begin somewhere (a tile's first
+// key takes a look at every row): a warp per tile.
+constexpr int kEntryThreads = 256;
+__global__ void __launch_bounds__(kEntryThreads) entries_kernel(CacheAttn p) {
+  ptx::griddep_wait();
+  ptx::griddep_launch_dependents();
+  const int lane = threadIdx.x % 32;
+  const int32_t i = blockIdx.x * (kEntryThreads / 32) + threadIdx.x / 32;
+  if (i >= p.entries) return;
+  AttnEntry e = attn_entry(p, i);
+  int32_t first = 0;
+  if (p.begin) {
+    first = 0x7fffffff;
+    for (int32_t t = lane; t < e.count; t += 32) first = min(first, max(p.begin[e.row0 + t], 0));
+    first = __reduce_min_sync(0xffffffffu, first);
+  }
+  attn_blocks(p, e, first);
+  if (lane == 0) p.entries_global[i] = e;
+}
+
+// The line of more tiles than a CTA's shared memory keeps.
 __global__ void __launch_bounds__(kLineThreads, 1) line_kernel(CacheAttn p) {
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
-  for (int32_t i = warp; i < p.entries; i += kLineThreads / 32) {
-    AttnEntry e = attn_entry(p, i);
-    int32_t first = 0;
-    if (p.begin) {
-      first = 0x7fffffff;
-      for (int32_t t = lane; t < e.count; t += 32) first = min(first, max(p.begin[e.row0 + t], 0));
-      first = __reduce_min_sync(0xffffffffu, first);
-    }
-    attn_blocks(p, e, first);
-    if (lane == 0) p.entries_global[i] = e;
-  }
-  __syncthreads();
-  __shared__ int64_t sums[kLineThreads / 32];
-  int64_t base = 0;
+  __shared__ uint64_t sums[kLineThreads / 32];
+  uint64_t base = 0;
   for (int32_t i0 = 0; i0 < p.entries; i0 += kLineThreads) {
     const int32_t i = i0 + (int32_t)threadIdx.x;
-    const int64_t cost = i < p.entries ? attn_cost(p.entries_global[i]) : 0;
-    int64_t incl = cost;
+    const uint32_t cost = i < p.entries ? attn_cost(p, p.entries_global[i]) : 0u;
+    uint32_t incl = cost;  // (of 32 tiles: 32 bits)
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const int64_t up = __shfl_up_sync(0xffffffffu, incl, o);
+      const uint32_t up = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += up;
     }
     if (lane == 31) sums[warp] = incl;
     __syncthreads();
-    int64_t before = base, total = 0;
+    uint64_t before = base, total = 0;
     for (int w = 0; w < kLineThreads / 32; ++w) {
       if (w < warp) before += sums[w];
       total += sums[w];
     }
-    if (i < p.entries) p.line_global[i] = before + incl - cost;
+    if (i < p.entries) p.line_global[i] = (int64_t)(before + incl - cost);
     base += total;
     __syncthreads();
   }
-  if (threadIdx.x == 0) p.line_global[p.entries] = base;
+  if (threadIdx.x == 0) p.line_global[p.entries] = (int64_t)base;
 }
 
 template <typename T>
@@ -186,7 +193,7 @@ __global__ void __launch_bounds__(kGenThreads) general_kernel(const CacheAttn p)
 #pragma unroll
       for (int c = 0; c < NV; ++c) acc[i][c] = 0.f;
     }
-    const int32_t blk0 = e.blk0 + walk.block0(), blocks = e.blocks > 0 ? walk.blocks() : 0;
+    const int32_t blk0 = e.blk0 + walk.block0(p), blocks = e.blocks > 0 ? walk.blocks(p) : 0;
     const int32_t last_key = min(e.L, p.causal ? max(e.pos0 + e.count, e.prefix) : e.L);  // one past the last that any row sees
     auto load = [&](int32_t b) {
       const uint32_t dst = kv_addr + (b & 1) * 2 * block_bytes;
@@ -334,7 +341,7 @@ enum class Kind { kGeneral, kMma, kFew, kUmma };
 struct Choice {
   Kind kind;
   int32_t group, per_kv, heads;  // query heads per tile row, such groups per key head, groups in all
-  int32_t rows_per_tile, tile_rows, block, min_units, grid;
+  int32_t rows_per_tile, tile_rows, block, min_units, extra, grid;
   int64_t entries;
   bool by_request;  // no request has more than one tile
 };
@@ -344,7 +351,8 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H) {
   int32_t most = 16;
   x.kind = Kind::kGeneral;
   x.block = kGenKeys;
-  x.min_units = 2;
+  x.min_units = 4;
+  x.extra = 2;
   if (c->dtype == ROCS_BF16 && kernel_path() == ROCS_PATH_AUTO && (c->dh == 32 || c->dh == 64 || c->dh == 128)) {
     x.kind = Kind::kMma;
     x.block = kMmaKeys;
@@ -357,6 +365,8 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H) {
     if ((int64_t)plan->largest * g > 64 && attn_umma_supported(c->dh, c->page)) {
       x.kind = Kind::kUmma;
       x.block = kUmmaKeys;
+      x.min_units = 8;
+      x.extra = 4;
       most = 128;  // of a side
     }
   }
@@ -468,6 +478,9 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
   p.slopes = slopes;
   p.block = x.block;
   p.min_units = x.min_units;
+  p.extra = x.extra;
+  p.light_rows = x.kind == Kind::kUmma ? x.rows_per_tile / 2 : x.rows_per_tile;
+  p.heavy = 2;
   p.tile_rows = x.tile_rows;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   p.meta = reinterpret_cast<AttnMeta*>(ws + w.meta);
@@ -482,7 +495,13 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
     if (st != ROCS_OK) return st;
     p.tiles = tiles.dev;
   }
-  p.listed = x.entries > kLocalEntries || (begin && x.rows_per_tile > 8);
+  p.listed = x.entries > kLocalEntries;
+  p.entries_made = p.listed || (begin && x.rows_per_tile > 8);
+  if (p.entries_made) {
+    const int64_t ctas = (x.entries + kEntryThreads / 32 - 1) / (kEntryThreads / 32);
+    const rocs_status_t st = launch_dependent(entries_kernel, dim3((unsigned)ctas), kEntryThreads, 0, stream, p);
+    if (st != ROCS_OK) return st;
+  }
   if (p.listed) {
     const rocs_status_t st = launch_dependent(line_kernel, dim3(1), kLineThreads, 0, stream, p);
     if (st != ROCS_OK) return st;

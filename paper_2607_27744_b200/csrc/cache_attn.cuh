@@ -5,7 +5,9 @@
 // key blocks (one if it has none: zeros are written).  All tiles of the launch stand in a line, tile by tile and inside
 // one block by block, and the line is cut into as many equal pieces as there are CTAs: every CTA gets the same number of
 // blocks whatever the lengths, which only the device knows.  A tile that a cut goes through leaves unnormalised parts in
-// the workspace, and a second small kernel joins them in the order of the keys.  At most two parts per CTA.
+// the workspace, and a second small kernel joins them in the order of the keys.  At most two parts per CTA.  What a tile takes
+// beside its blocks (loading Q, the last products, writing O) counts as blocks too: tiles of few keys would make some CTAs
+// late.
 #pragma once
 #include <cuda_bf16.h>
 
@@ -51,12 +53,14 @@ struct CacheAttn {
   // scores in units of 1 / unit powers of two: scale * log2(e) / unit; capped: scale / cap, then cap * log2(e) / unit
   float scale, cap, unit;
   const float* slopes;
-  int32_t block, min_units; // keys per unit, least units of a CTA
+  int32_t block, min_units; // keys of a block, least units of a CTA
+  int32_t extra;            // units of a tile beside its blocks'
+  int32_t light_rows, heavy;  // a block weighs 1 in a tile of up to so many batch rows, otherwise `heavy`
   int32_t tile_rows;        // rows of a tile as the parts hold them (batch rows x group, rounded up)
   // workspace
   int64_t* line_global;     // [entries + 1]
   AttnEntry* entries_global;
-  bool listed;              // the two above were made by a launch in front
+  bool entries_made, listed;  // the entries, and the line too, were made by launches in front
   AttnMeta* meta;           // [CTAs]
   float* parts;             // [2 CTAs][tile_rows][dh], then [2 CTAs][tile_rows][2]: reference and sum
   uint32_t* status;
@@ -120,13 +124,21 @@ __device__ __forceinline__ void attn_blocks(const CacheAttn& p, AttnEntry& e, in
   e.blk0 = first_key / p.block;
   e.blocks = last > first_key ? (last + p.block - 1) / p.block - e.blk0 : 0;
 }
-__device__ __forceinline__ int64_t attn_cost(const AttnEntry& e) { return e.count > 0 ? max(e.blocks, 1) : 0; }
+// Units of a tile: `extra` for its beginning and end, and a block's weight for each block.
+__device__ __forceinline__ int32_t attn_weight(const CacheAttn& p, const AttnEntry& e) { return e.count > p.light_rows ? p.heavy : 1; }
+__device__ __forceinline__ uint32_t attn_cost(const CacheAttn& p, const AttnEntry& e) {
+  return e.count > 0 ? (uint32_t)(p.extra + max(e.blocks, 1) * attn_weight(p, e)) : 0u;
+}
 
 // The line, found by the CTA's THREADS threads (all call this) or by the launch in front.
 template <int THREADS>
 __device__ __forceinline__ AttnLineView attn_line(const CacheAttn& p, AttnLine& mem) {
   if (p.listed) return AttnLineView{p.line_global, p.entries_global};
   for (int32_t i = threadIdx.x; i < p.entries; i += THREADS) {
+    if (p.entries_made) {
+      mem.entry[i] = p.entries_global[i];
+      continue;
+    }
     AttnEntry e = attn_entry(p, i);
     int32_t first = 0;
     if (p.begin) {
@@ -141,7 +153,7 @@ __device__ __forceinline__ AttnLineView attn_line(const CacheAttn& p, AttnLine& 
   static_assert(kLocalEntries == 128 && THREADS >= 128, "four warps of entries");
   uint32_t cost = 0, incl = 0;
   if (threadIdx.x < kLocalEntries) {
-    cost = (int32_t)threadIdx.x < p.entries ? (uint32_t)attn_cost(mem.entry[threadIdx.x]) : 0u;
+    cost = (int32_t)threadIdx.x < p.entries ? attn_cost(p, mem.entry[threadIdx.x]) : 0u;
     incl = cost;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -165,11 +177,26 @@ __device__ __forceinline__ AttnLineView attn_line(const CacheAttn& p, AttnLine& 
 struct AttnWalk {
   int64_t u, end;      // units
   int64_t tile_begin;  // unit at which the tile at hand begins
-  int32_t entry, head, cost;
+  int32_t entry, head, cost, weight;
   bool first;          // the piece at hand is the CTA's first
-  // x / d for d < 2^31; most lines are short enough for one instruction's worth of division
+  // x / d for 0 < d < 2^31; most lines are short enough for one instruction's worth of division
   __device__ __forceinline__ static int64_t over(int64_t x, int32_t d) {
     return x >> 32 == 0 ? (int64_t)((uint32_t)x / (uint32_t)d) : x / d;
+  }
+  // The tile that unit x < total is in, and x moved down to where a piece may begin: the tile's first unit, or a block.
+  __device__ __forceinline__ int64_t find(const CacheAttn& p, const AttnLineView& v, int64_t x) {
+    int32_t lo = 0, hi = p.entries;  // largest entry that begins at or before x
+    while (hi - lo > 1) {
+      const int32_t mid = lo + (hi - lo) / 2;
+      if (v.line[mid] * p.heads <= x) lo = mid; else hi = mid;
+    }
+    entry = lo;
+    cost = (int32_t)(v.line[lo + 1] - v.line[lo]);
+    head = (int32_t)over(x - v.line[lo] * p.heads, cost);
+    tile_begin = v.line[lo] * p.heads + (int64_t)head * cost;
+    weight = attn_weight(p, v.entry[lo]);
+    const int32_t block = ((int32_t)(x - tile_begin) - p.extra) / weight;
+    return block <= 0 ? tile_begin : tile_begin + p.extra + block * weight;
   }
   // false: nothing for this CTA.  Its thread NOTER, one that has little else to do, notes what the joining kernel needs.
   template <int NOTER>
@@ -187,51 +214,48 @@ struct AttnWalk {
     const int64_t each = over(total, ctas);
     const int32_t more = (int32_t)(total - each * ctas);
     auto cut = [&](int32_t x) { return each * x + min(x, more); };
-    u = cut(i);
-    end = cut(i + 1);
-    int32_t lo = 0, hi = p.entries;  // largest entry that begins at or before u
-    while (hi - lo > 1) {
-      const int32_t mid = lo + (hi - lo) / 2;
-      if (v.line[mid] * p.heads <= u) lo = mid; else hi = mid;
-    }
-    entry = lo;
-    cost = (int32_t)(v.line[lo + 1] - v.line[lo]);
-    const int64_t in = u - v.line[lo] * p.heads;
-    head = (int32_t)over(in, cost);
-    tile_begin = v.line[lo] * p.heads + (int64_t)head * cost;
+    end = i + 1 < ctas ? find(p, v, cut(i + 1)) : total;
+    u = find(p, v, cut(i));
     if (threadIdx.x == NOTER) {
       AttnMeta m;
       m.parts = 0;
-      if (u > tile_begin) {
+      if (u > tile_begin && u < end) {
+        // the CTA in front began the tile if it is cut in front of the tile's second block, and it was its first piece if it
+        // is not cut in front of the tile
         const int64_t in_front = cut(i - 1), last = tile_begin + cost - 1;
-        if (in_front <= tile_begin) {
+        if (in_front < tile_begin + p.extra + weight) {
           m.entry = v.entry[entry];
           m.head = head;
-          const int64_t longer = (each + 1) * more;  // units of those CTAs; the one that has unit `last`:
+          const int64_t longer = (each + 1) * more;  // units of the longer CTAs; the one that has unit `last`:
           const int32_t at = last < longer ? (int32_t)(last / (each + 1)) : more + (int32_t)((last - longer) / each);
           m.parts = at - (i - 1) + 1;
-          m.place = 2 * (i - 1) + (in_front == tile_begin ? 0 : 1);
+          m.place = 2 * (i - 1) + (in_front >= tile_begin ? 0 : 1);
         }
       }
       p.meta[i] = m;
     }
-    return true;
+    return u < end;
   }
   __device__ __forceinline__ bool more() const { return u < end; }
-  __device__ __forceinline__ int32_t block0() const { return (int32_t)(u - tile_begin); }
-  __device__ __forceinline__ int32_t blocks() const { return (int32_t)(min(end, tile_begin + cost) - u); }
+  __device__ __forceinline__ int32_t block0(const CacheAttn& p) const {
+    return u == tile_begin ? 0 : ((int32_t)(u - tile_begin) - p.extra) / weight;
+  }
+  __device__ __forceinline__ int32_t blocks(const CacheAttn& p) const {
+    return ((int32_t)(min(end, tile_begin + cost) - tile_begin) - p.extra) / weight - block0(p);
+  }
   __device__ __forceinline__ bool whole() const { return u == tile_begin && end >= tile_begin + cost; }
   // where a part goes: a CTA's first piece to its first place, otherwise (its last) to the second
   __device__ __forceinline__ int32_t part() const { return 2 * (int32_t)blockIdx.x + (first ? 0 : 1); }
   __device__ __forceinline__ void next(const CacheAttn& p, const AttnLineView& v) {
-    u += blocks();
+    tile_begin += cost;
+    u = tile_begin;
     first = false;
     if (u >= end) return;
-    tile_begin += cost;
     if (++head == p.heads) {
       head = 0;
       do ++entry; while (v.line[entry + 1] == v.line[entry]);
       cost = (int32_t)(v.line[entry + 1] - v.line[entry]);
+      weight = attn_weight(p, v.entry[entry]);
     }
   }
 };

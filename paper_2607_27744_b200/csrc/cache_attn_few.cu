@@ -123,7 +123,7 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
     for (; ok && walk.more(); walk.next(p, view)) {
       const AttnEntry e = view.entry[walk.entry];
       if (e.blocks == 0) continue;
-      const int32_t blk0 = e.blk0 + walk.block0(), n = walk.blocks(), kv_head = walk.head / p.per_kv;
+      const int32_t blk0 = e.blk0 + walk.block0(p), n = walk.blocks(p), kv_head = walk.head / p.per_kv;
       const int32_t* row = p.table + (int64_t)e.slot * p.width;
       auto look_up = [&](int32_t b) {  // page of this lane's box of block b; none behind the slot's end: zeros
         const int32_t j = (blk0 + b) * kFewKeys + lane * box_rows;
@@ -245,7 +245,7 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
       for (int t = 0; t < DH / 16; ++t)
 #pragma unroll
         for (int c = 0; c < 4; ++c) o[n][t][c] = 0.f;
-    const int32_t blk0 = e.blk0 + walk.block0(), blocks = e.blocks > 0 ? walk.blocks() : 0;
+    const int32_t blk0 = e.blk0 + walk.block0(p), blocks = e.blocks > 0 ? walk.blocks(p) : 0;
     for (int32_t b = 0; b < blocks; ++b) {
       const uint32_t st = it % C::kStages;
       const bool there = mbar_wait_paced(sb + C::kFull + 8 * st, (it / C::kStages) & 1, abort_flag, p.status, kStatusFew | 3);

@@ -84,9 +84,9 @@ __global__ void __launch_bounds__(kMmaThreads, MmaCfg<DH>::kPerSm) mma_kernel(co
       const AttnEntry& e = view.entry[ahead.entry];
       if (e.blocks > 0) {
         ahead_b = 0;
-        ahead_n = ahead.blocks();
+        ahead_n = ahead.blocks(p);
         ahead_slot = e.slot;
-        ahead_blk0 = e.blk0 + ahead.block0();
+        ahead_blk0 = e.blk0 + ahead.block0(p);
         ahead_last = min(e.L, p.causal ? max(e.pos0 + e.count, e.prefix) : e.L);
         ahead_head = (int64_t)(ahead.head / p.per_kv) * p.head_bytes + load_chunk * 16;
         return;
@@ -163,7 +163,7 @@ __global__ void __launch_bounds__(kMmaThreads, MmaCfg<DH>::kPerSm) mma_kernel(co
     for (int n = 0; n < DH / 8; ++n)
 #pragma unroll
       for (int c = 0; c < 4; ++c) o[n][c] = 0.f;
-    const int32_t blk0 = e.blk0 + walk.block0(), blocks = e.blocks > 0 ? walk.blocks() : 0;
+    const int32_t blk0 = e.blk0 + walk.block0(p), blocks = e.blocks > 0 ? walk.blocks(p) : 0;
     for (int32_t b = 0; b < blocks; ++b) {
       cp_async_wait<C::kStages - 2>();
       __syncthreads();  // the block is there for all, and all are done with the one whose place the next load takes

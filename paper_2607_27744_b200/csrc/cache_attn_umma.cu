@@ -186,7 +186,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
     for (; ok && walk.more(); walk.next(p, view)) {
       const AttnEntry e = view.entry[walk.entry];
       if (e.blocks == 0) continue;
-      const int32_t blk0 = e.blk0 + walk.block0(), n = walk.blocks(), kv_head = walk.head / p.per_kv;
+      const int32_t blk0 = e.blk0 + walk.block0(p), n = walk.blocks(p), kv_head = walk.head / p.per_kv;
       const int32_t* row = p.table + (int64_t)e.slot * p.width;
       auto look_up = [&](int32_t b) {  // page of this lane's box of block b; none behind the slot's end: zeros
         const int32_t j = (blk0 + b) * BK + lane * box_rows;
@@ -297,7 +297,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       for (; ok && walk.more(); walk.next(p, view)) {
         const AttnEntry e = view.entry[walk.entry];
         if (e.blocks == 0) continue;
-        const int32_t n = walk.blocks();
+        const int32_t n = walk.blocks(p);
         if (!wait(sb + C::kQFull, n_piece & 1, 5)) break;
         ++n_piece;
         if (e.count > per_side) {  // two sides, every block for both
@@ -399,7 +399,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       // rows that do not exist ask for no mask
       const int32_t lo_most = __reduce_max_sync(0xffffffffu, there ? keys.lo : 0);
       const int32_t hi_least = __reduce_min_sync(0xffffffffu, there ? keys.hi : 0x7fffffff);
-      const int32_t blk0 = e.blk0 + walk.block0(), n = walk.blocks();
+      const int32_t blk0 = e.blk0 + walk.block0(p), n = walk.blocks(p);
       const int32_t step = split ? 2 : 1, first = split ? side : 0;
       float m = sees ? -INFINITY : 0.f, l = 0.f;  // -inf: no reference yet
       float own[2] = {0.f, 0.f};  // this half's sums of the last two blocks
