@@ -36,7 +36,6 @@ constexpr int kUmmaThreads = 20 * 32;
 constexpr int kSide = 128;               // rows of a side = tensor memory lanes
 constexpr int BK = kUmmaKeys;
 constexpr uint32_t kStatusCache = 0x500;
-constexpr int kOnFma = 3;  // of eight pairs of exponentials
 constexpr float kMoveAt = 1099511627776.f;  // 2^40
 
 template <int DH_>
@@ -84,6 +83,27 @@ __device__ __forceinline__ void umma_ts(uint32_t d_tmem, uint32_t a_tmem, uint64
       "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// A wait that leaves the issue slots to the other warps: a probe may be suspended until the phase completes (0.2 ms at most,
+// so that the abort flag is seen).  The softmax waits a good part of a block, and probes that come back at once, with a look
+// at the clock between two, cost the long chunk 8 % on a GPU that has not come to its power limit.
+__device__ __forceinline__ bool mbar_wait_suspended(uint32_t bar, uint32_t parity, AbortFlag* abort_flag, uint32_t* status, uint32_t code) {
+  const uint64_t t0 = globaltimer_ns();
+  while (true) {
+    uint32_t ok;
+    asm volatile(
+        "{\n.reg .pred p;\nmbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\nselp.u32 %0, 1, 0, p;\n}\n"
+        : "=r"(ok)
+        : "r"(bar), "r"(parity), "r"(200000u)
+        : "memory");
+    if (ok) return true;
+    if (abort_flag->v) return false;
+    if (globaltimer_ns() - t0 > kWaitLimitNs) {
+      abort_flag->v = 1;
+      atomicCAS(status, 0u, code);
+      return false;
+    }
+  }
+}
 __device__ __forceinline__ void tmem_st_x8(uint32_t taddr, const uint32_t* r) {
   asm volatile("tcgen05.st.sync.aligned.32x32b.x8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"r"(taddr), "r"(r[0]), "r"(r[1]),
                "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7])
@@ -93,6 +113,39 @@ __device__ __forceinline__ uint64_t fadd2(uint64_t a, uint64_t b) {
   uint64_t d;
   asm("add.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
+}
+
+__device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
+  uint64_t d;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
+  return d;
+}
+// tanh of a pair within [-1, 1]: t P(t^2), fitted for the least absolute error, 2.8e-6 (two instructions of the
+// special-function unit per value and a third for its weight would be three times what the kernel waits for without a cap).
+__device__ __forceinline__ uint64_t tanh_pair(uint64_t t) {
+  const uint64_t u = fmul2(t, t);
+  uint64_t r = ffma2(u, pack2(0.00836588628590107f, 0.00836588628590107f), pack2(-0.04329986497759819f, -0.04329986497759819f));
+  r = ffma2(r, u, pack2(0.12922066450119019f, 0.12922066450119019f));
+  r = ffma2(r, u, pack2(-0.33265823125839233f, -0.33265823125839233f));
+  r = ffma2(r, u, pack2(0.9999684691429138f, 0.9999684691429138f));
+  return fmul2(r, t);
+}
+// Four lanes with four 16-byte pieces of a row each: lane c of them gets piece c of all four rows, so that a store of the warp
+// touches 8 rows with 64 bytes each and not 32 with 16.
+__device__ __forceinline__ void swap_pieces(uint4& mine, uint4& other, bool upper, int distance) {
+  const uint4 give = upper ? mine : other;
+  uint4 got;
+  got.x = __shfl_xor_sync(0xffffffffu, give.x, distance);
+  got.y = __shfl_xor_sync(0xffffffffu, give.y, distance);
+  got.z = __shfl_xor_sync(0xffffffffu, give.z, distance);
+  got.w = __shfl_xor_sync(0xffffffffu, give.w, distance);
+  if (upper) mine = got; else other = got;
+}
+__device__ __forceinline__ void transpose_pieces(uint4 (&v)[4], int lane) {
+  swap_pieces(v[0], v[1], lane & 1, 1);
+  swap_pieces(v[2], v[3], lane & 1, 1);
+  swap_pieces(v[0], v[2], lane & 2, 2);
+  swap_pieces(v[1], v[3], lane & 2, 2);
 }
 
 // 2^x for a pair on the FMA pipes: 2^n 2^f with n the nearest integer and a polynomial of degree 3 for 2^f on [-1/2, 1/2]
@@ -415,21 +468,40 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
           if (most > kMoveAt * moved) up = (float)((int32_t)(__float_as_uint(most / moved) >> 23) - 127);
         }
         const bool slow = __any_sync(0xffffffffu, m == -INFINITY || up != 0.f);
-        if (!mbar_wait_paced(sb + C::kSFull + 8 * side, cnt_s & 1, abort_flag, p.status, kStatusCache | 10)) { aborted = true; break; }
+        if (!mbar_wait_suspended(sb + C::kSFull + 8 * side, cnt_s & 1, abort_flag, p.status, kStatusCache | 10)) { aborted = true; break; }
         tc_fence_after_sync();
         const int32_t b0 = (blk0 + n - 1 - i) * BK, j0 = b0 + half * 64;  // the block's first key, this thread's
         const bool all_begun = b0 >= lo_most, none_ended = b0 + BK <= hi_least;  // what masks may be left out
-        // scores of columns c0.. in log2 units but for the plain scale, -inf where the row does not see the key
+        // scores of columns c0.. in log2 units but for a factor (`scale`), -inf where the row does not see the key
+        const float scale = BIAS ? 1.f : CAP ? p.cap : p.scale;
         auto scores = [&](int c0, uint32_t (&s)[16]) {
-          if (CAP || BIAS) {
-            const float away = (float)(keys.pos - j0 - c0);
+          if (CAP) {
+            uint64_t t[8];
+            float most = 0.f;
 #pragma unroll
-            for (int x = 0; x < 16; ++x) {
-              float v = __uint_as_float(s[x]) * p.scale;
-              if (CAP) v = p.cap * tanh_fast(v);
-              if (BIAS) v = fmaf(-slope, fabsf(away - (float)x), v);
-              s[x] = __float_as_uint(v);
+            for (int x = 0; x < 8; ++x) {
+              t[x] = fmul2(pack2(__uint_as_float(s[2 * x]), __uint_as_float(s[2 * x + 1])), pack2(p.scale, p.scale));
+              float t0, t1;
+              unpack2(t[x], t0, t1);
+              most = fmaxf(most, fmaxf(fabsf(t0), fabsf(t1)));
             }
+#pragma unroll
+            for (int x = 0; x < 8; ++x) {
+              float t0, t1;
+              unpack2(most <= 1.f ? tanh_pair(t[x]) : t[x], t0, t1);
+              s[2 * x] = __float_as_uint(t0);
+              s[2 * x + 1] = __float_as_uint(t1);
+            }
+            if (!(most <= 1.f)) {  // a row's own way, whatever the others take
+#pragma unroll
+              for (int x = 0; x < 16; ++x) s[x] = __float_as_uint(tanh_fast(__uint_as_float(s[x])));
+            }
+          }
+          if (BIAS) {
+            const float away = (float)(keys.pos - j0 - c0), factor = CAP ? p.cap : p.scale;
+#pragma unroll
+            for (int x = 0; x < 16; ++x)
+              s[x] = __float_as_uint(fmaf(-slope, fabsf(away - (float)x), __uint_as_float(s[x]) * factor));
           }
           if (!all_begun) {
             const int32_t lo = keys.lo - j0 - c0;
@@ -444,7 +516,6 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
               if (x >= hi) s[x] = 0xff800000u;
           }
         };
-        const float scale = CAP || BIAS ? 1.f : p.scale;
         if (slow) {
           if (__any_sync(0xffffffffu, m == -INFINITY)) {  // rows without a reference: the maximum of this block
             float mx = -INFINITY;
@@ -484,44 +555,38 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
         uint32_t s[2][16];
         tmem_ld_32x32b_x16(t_s, s[0]);
         tmem_ld_wait();
-        // `some`: how many of eight pairs take the FMA pipes instead of the special-function unit, whose 16 results a cycle
-        // would be what the kernel waits for
-        auto weights = [&](int c, auto some) {
-          uint32_t pk[8];
+        // `some`: how many of eight pairs take the FMA pipes instead of the special-function unit.  With heads of 64 a block's
+        // exponentials take twice as long as its products (candidates of 32 requests: 127 us without, 122 us with two of
+        // eight, 128 us with four); with heads of 128 the same time (long chunk: 479 us without, 484 us with two).
+        auto weights = [&](auto some) {
 #pragma unroll
-          for (int x = 0; x < 16; x += 2) {
-            const uint64_t x2 = ffma2(pack2(__uint_as_float(s[c % 2][x]), __uint_as_float(s[c % 2][x + 1])), c2, m2);
-            float p0, p1;
-            if ((x / 2 * 3) % 8 < decltype(some)::value) {
-              unpack2(exp2_pair(x2), p0, p1);
-            } else {
-              float x0, x1;
-              unpack2(x2, x0, x1);
-              p0 = ex2_approx(x0);
-              p1 = ex2_approx(x1);
+          for (int c = 0; c < 4; ++c) {
+            if (c > 0) tmem_ld_wait();
+            if (c < 3) tmem_ld_32x32b_x16(t_s + (c + 1) * 16, s[(c + 1) % 2]);
+            scores(c * 16, s[c % 2]);
+            uint32_t pk[8];
+#pragma unroll
+            for (int x = 0; x < 16; x += 2) {
+              const uint64_t x2 = ffma2(pack2(__uint_as_float(s[c % 2][x]), __uint_as_float(s[c % 2][x + 1])), c2, m2);
+              float p0, p1;
+              if ((x / 2 * 3) % 8 < decltype(some)::value) {
+                unpack2(exp2_pair(x2), p0, p1);
+              } else {
+                float x0, x1;
+                unpack2(x2, x0, x1);
+                p0 = ex2_approx(x0);
+                p1 = ex2_approx(x1);
+              }
+              sum2 = fadd2(sum2, pack2(p0, p1));
+              pk[x / 2] = bf16_pair(p0, p1);
             }
-            sum2 = fadd2(sum2, pack2(p0, p1));
-            pk[x / 2] = bf16_pair(p0, p1);
+            tmem_st_x8(t_s + c * 8, pk);
           }
-          tmem_st_x8(t_s + c * 8, pk);
         };
-        if (all_begun && none_ended) {
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (c > 0) tmem_ld_wait();
-            if (c < 3) tmem_ld_32x32b_x16(t_s + (c + 1) * 16, s[(c + 1) % 2]);
-            scores(c * 16, s[c % 2]);
-            weights(c, std::integral_constant<int, kOnFma>());
-          }
-        } else {  // (a masked key's weight is 0 from the special-function unit, not 2^-125)
-#pragma unroll
-          for (int c = 0; c < 4; ++c) {
-            if (c > 0) tmem_ld_wait();
-            if (c < 3) tmem_ld_32x32b_x16(t_s + (c + 1) * 16, s[(c + 1) % 2]);
-            scores(c * 16, s[c % 2]);
-            weights(c, std::integral_constant<int, 0>());
-          }
-        }
+        // blocks without a mask on code of their own (long chunk: 531 us on one for both) where scores are not capped (first
+        // visits: 175 us on one, 186 us on two)
+        if (!CAP && all_begun && none_ended) weights(std::integral_constant<int, DH == 64 ? 2 : 0>());
+        else weights(std::integral_constant<int, 0>());  // (a masked key's weight is 0 there, not 2^-125)
         float s0, s1;
         unpack2(sum2, s0, s1);
         own[cnt_s & 1] = sees ? s0 + s1 : 0.f;
@@ -573,39 +638,66 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       // non-finite, or only scores of -inf, which exp2_pair does not take to 0: by hand
       float probe = m == -INFINITY && l != 0.f ? NAN : l * 0.f;
       float* to = attn_part(p, part) + (int64_t)tile_row * DH + col0;
+      const uint32_t rows_there = __ballot_sync(0xffffffffu, there);
+      const int lane4 = lane & 3, lane0 = lane & ~3;
+      uint8_t* out4[4];  // the rows of this lane and its three neighbours
+#pragma unroll
+      for (int k = 0; k < 4; ++k)
+        out4[k] = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(out), lane0 + k));
+      auto column = [&](uint32_t a, uint32_t b) {  // of the row's result
+        float v = __uint_as_float(a);
+        probe = fmaf(v, 0.f, probe);
+        v *= wa;
+        if (both) {
+          probe = fmaf(__uint_as_float(b), 0.f, probe);
+          v = fmaf(__uint_as_float(b), wb, v);
+        }
+        return v * inv;
+      };
 #pragma unroll 1
       for (int c = 0; c < width; c += 16) {
         uint32_t o[16], ob[16];
         tmem_ld_32x32b_x16(t_a + c, o);
         if (both) tmem_ld_32x32b_x16(t_b + c, ob);
         tmem_ld_wait();
+        uint4 v[4];
+        if (whole) {  // 16 columns: two pieces, and with the next 16 of a wide share four
 #pragma unroll
-        for (int x = 0; x < 16; ++x) {
-          float v = __uint_as_float(o[x]);
-          probe = fmaf(v, 0.f, probe);
-          v *= wa;
-          if (both) {
-            probe = fmaf(__uint_as_float(ob[x]), 0.f, probe);
-            v = fmaf(__uint_as_float(ob[x]), wb, v);
+          for (int x = 0; x < 2; ++x)
+            v[x] = make_uint4(bf16_pair(column(o[8 * x], ob[8 * x]), column(o[8 * x + 1], ob[8 * x + 1])),
+                              bf16_pair(column(o[8 * x + 2], ob[8 * x + 2]), column(o[8 * x + 3], ob[8 * x + 3])),
+                              bf16_pair(column(o[8 * x + 4], ob[8 * x + 4]), column(o[8 * x + 5], ob[8 * x + 5])),
+                              bf16_pair(column(o[8 * x + 6], ob[8 * x + 6]), column(o[8 * x + 7], ob[8 * x + 7])));
+          if (width == 16) {
+            if (there) {
+              *reinterpret_cast<uint4*>(out + col0 * 2) = v[0];
+              *reinterpret_cast<uint4*>(out + col0 * 2 + 16) = v[1];
+            }
+            continue;
           }
-          o[x] = __float_as_uint(v * inv);
-        }
-        if (!there) continue;
-        if (whole) {
+          c += 16;
+          tmem_ld_32x32b_x16(t_a + c, o);
+          if (both) tmem_ld_32x32b_x16(t_b + c, ob);
+          tmem_ld_wait();
 #pragma unroll
-          for (int x = 0; x < 16; x += 8) {
-            uint4 w;
-            w.x = bf16_pair(__uint_as_float(o[x]), __uint_as_float(o[x + 1]));
-            w.y = bf16_pair(__uint_as_float(o[x + 2]), __uint_as_float(o[x + 3]));
-            w.z = bf16_pair(__uint_as_float(o[x + 4]), __uint_as_float(o[x + 5]));
-            w.w = bf16_pair(__uint_as_float(o[x + 6]), __uint_as_float(o[x + 7]));
-            *reinterpret_cast<uint4*>(out + (col0 + c + x) * 2) = w;
-          }
+          for (int x = 0; x < 2; ++x)
+            v[2 + x] = make_uint4(bf16_pair(column(o[8 * x], ob[8 * x]), column(o[8 * x + 1], ob[8 * x + 1])),
+                                  bf16_pair(column(o[8 * x + 2], ob[8 * x + 2]), column(o[8 * x + 3], ob[8 * x + 3])),
+                                  bf16_pair(column(o[8 * x + 4], ob[8 * x + 4]), column(o[8 * x + 5], ob[8 * x + 5])),
+                                  bf16_pair(column(o[8 * x + 6], ob[8 * x + 6]), column(o[8 * x + 7], ob[8 * x + 7])));
+          transpose_pieces(v, lane);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if ((rows_there >> (lane0 + k)) & 1) *reinterpret_cast<uint4*>(out4[k] + (col0 + c - 16) * 2 + lane4 * 16) = v[k];
         } else {
 #pragma unroll
-          for (int x = 0; x < 16; x += 4)
-            *reinterpret_cast<float4*>(to + c + x) = make_float4(__uint_as_float(o[x]), __uint_as_float(o[x + 1]), __uint_as_float(o[x + 2]),
-                                                                 __uint_as_float(o[x + 3]));
+          for (int x = 0; x < 4; ++x)
+            v[x] = make_uint4(__float_as_uint(column(o[4 * x], ob[4 * x])), __float_as_uint(column(o[4 * x + 1], ob[4 * x + 1])),
+                              __float_as_uint(column(o[4 * x + 2], ob[4 * x + 2])), __float_as_uint(column(o[4 * x + 3], ob[4 * x + 3])));
+          transpose_pieces(v, lane);
+#pragma unroll
+          for (int k = 0; k < 4; ++k)
+            if ((rows_there >> (lane0 + k)) & 1) *reinterpret_cast<uint4*>(to + (lane0 + k - lane) * DH + c + lane4 * 4) = v[k];
         }
       }
       const bool leads = half == 0 && (!split || side == 0);  // of the threads of a row
