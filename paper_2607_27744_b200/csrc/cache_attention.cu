@@ -351,8 +351,8 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H) {
   int32_t most = 16;
   x.kind = Kind::kGeneral;
   x.block = kGenKeys;
-  x.min_units = 4;
-  x.extra = 2;
+  x.min_units = 2;
+  x.extra = 1;
   if (c->dtype == ROCS_BF16 && kernel_path() == ROCS_PATH_AUTO && (c->dh == 32 || c->dh == 64 || c->dh == 128)) {
     x.kind = Kind::kMma;
     x.block = kMmaKeys;
@@ -495,8 +495,8 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
     if (st != ROCS_OK) return st;
     p.tiles = tiles.dev;
   }
-  p.listed = x.entries > kLocalEntries;
-  p.entries_made = p.listed || (begin && x.rows_per_tile > 8);
+  p.listed = x.entries > kLocalLine;
+  p.entries_made = x.entries > kLocalEntries || (begin && x.rows_per_tile > 8);
   if (p.entries_made) {
     const int64_t ctas = (x.entries + kEntryThreads / 32 - 1) / (kEntryThreads / 32);
     const rocs_status_t st = launch_dependent(entries_kernel, dim3((unsigned)ctas), kEntryThreads, 0, stream, p);

@@ -16,7 +16,8 @@
 
 namespace rocs {
 
-constexpr int kLocalEntries = 128;  // up to this many tiles (without heads) every CTA finds the line itself
+constexpr int kLocalEntries = 128;  // up to this many tiles (without heads) every CTA finds them itself,
+constexpr int kLocalLine = 256;     // up to this many the line of tiles that a launch in front found
 
 // A run of rows of one request: everything a kernel has to know about it but the head.
 struct AttnEntry {
@@ -77,9 +78,9 @@ inline bool make_page_map(CUtensorMap* map, const void* base, const CacheAttn& p
 
 #ifdef __CUDACC__
 struct AttnLine {
-  int64_t line[kLocalEntries + 1];
+  int64_t line[kLocalLine + 1];
   AttnEntry entry[kLocalEntries];
-  uint32_t sums[kLocalEntries / 32];
+  uint32_t sums[kLocalLine / 32];
 };
 struct AttnLineView {
   const int64_t* line;
@@ -134,43 +135,51 @@ __device__ __forceinline__ uint32_t attn_cost(const CacheAttn& p, const AttnEntr
 template <int THREADS>
 __device__ __forceinline__ AttnLineView attn_line(const CacheAttn& p, AttnLine& mem) {
   if (p.listed) return AttnLineView{p.line_global, p.entries_global};
-  for (int32_t i = threadIdx.x; i < p.entries; i += THREADS) {
-    if (p.entries_made) {
-      mem.entry[i] = p.entries_global[i];
-      continue;
+  static_assert(kLocalLine % 32 == 0 && kLocalLine <= 2 * THREADS && THREADS >= kLocalEntries, "two tiles per thread");
+  const AttnEntry* entries = mem.entry;
+  if (p.entries_made) {
+    entries = p.entries_global;
+  } else {
+    if ((int32_t)threadIdx.x < p.entries) {
+      AttnEntry e = attn_entry(p, threadIdx.x);
+      int32_t first = 0;
+      if (p.begin) {
+        first = 0x7fffffff;
+        for (int32_t t = 0; t < e.count; ++t) first = min(first, max(p.begin[e.row0 + t], 0));
+      }
+      attn_blocks(p, e, first);
+      mem.entry[threadIdx.x] = e;
     }
-    AttnEntry e = attn_entry(p, i);
-    int32_t first = 0;
-    if (p.begin) {
-      first = 0x7fffffff;
-      for (int32_t t = 0; t < e.count; ++t) first = min(first, max(p.begin[e.row0 + t], 0));
-    }
-    attn_blocks(p, e, first);
-    mem.entry[i] = e;
+    __syncthreads();
   }
-  __syncthreads();
   // (a tile's cost is below 2^26: 32 of them stay in 32 bits)
-  static_assert(kLocalEntries == 128 && THREADS >= 128, "four warps of entries");
-  uint32_t cost = 0, incl = 0;
-  if (threadIdx.x < kLocalEntries) {
-    cost = (int32_t)threadIdx.x < p.entries ? attn_cost(p, mem.entry[threadIdx.x]) : 0u;
-    incl = cost;
+  uint32_t cost[2], incl[2];
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const int32_t i = threadIdx.x + r * THREADS;
+    cost[r] = i < p.entries ? attn_cost(p, entries[i]) : 0u;
+    incl[r] = cost[r];
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
-      const uint32_t up = __shfl_up_sync(0xffffffffu, incl, o);
-      if ((int)(threadIdx.x % 32) >= o) incl += up;
+      const uint32_t up = __shfl_up_sync(0xffffffffu, incl[r], o);
+      if ((int)(threadIdx.x % 32) >= o) incl[r] += up;
     }
-    if (threadIdx.x % 32 == 31) mem.sums[threadIdx.x / 32] = incl;
+    if (threadIdx.x % 32 == 31 && i < kLocalLine) mem.sums[i / 32] = incl[r];
   }
   __syncthreads();
-  if (threadIdx.x < kLocalEntries) {
-    int64_t base = 0;
-    for (int w = 0; w < (int)threadIdx.x / 32; ++w) base += mem.sums[w];
-    if ((int32_t)threadIdx.x <= p.entries) mem.line[threadIdx.x] = base + (incl - cost);
-    if ((int)threadIdx.x == kLocalEntries - 1 && p.entries == kLocalEntries) mem.line[kLocalEntries] = base + incl;
+#pragma unroll
+  for (int r = 0; r < 2; ++r) {
+    const int32_t i = threadIdx.x + r * THREADS;
+    if (i < kLocalLine && i < p.entries) {
+      int64_t base = 0;
+      for (int w = 0; w < i / 32; ++w) base += mem.sums[w];
+      mem.line[i] = base + (incl[r] - cost[r]);
+      if (i == p.entries - 1) mem.line[p.entries] = base + incl[r];
+    }
   }
+  if (p.entries == 0 && threadIdx.x == 0) mem.line[0] = 0;
   __syncthreads();
-  return AttnLineView{mem.line, mem.entry};
+  return AttnLineView{mem.line, entries};
 }
 
 // A CTA's way along its piece of the line.

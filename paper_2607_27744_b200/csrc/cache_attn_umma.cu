@@ -120,15 +120,21 @@ __device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
-// tanh of a pair within [-1, 1]: t P(t^2), fitted for the least absolute error, 2.8e-6 (two instructions of the
+// tanh of a pair within [-3/4, 3/4]: t P(t^2), fitted for the least absolute error, 3.6e-6 (two instructions of the
 // special-function unit per value and a third for its weight would be three times what the kernel waits for without a cap).
-__device__ __forceinline__ uint64_t tanh_pair(uint64_t t) {
-  const uint64_t u = fmul2(t, t);
-  uint64_t r = ffma2(u, pack2(0.00836588628590107f, 0.00836588628590107f), pack2(-0.04329986497759819f, -0.04329986497759819f));
-  r = ffma2(r, u, pack2(0.12922066450119019f, 0.12922066450119019f));
-  r = ffma2(r, u, pack2(-0.33265823125839233f, -0.33265823125839233f));
-  r = ffma2(r, u, pack2(0.9999684691429138f, 0.9999684691429138f));
+// `u` receives t^2.
+__device__ __forceinline__ uint64_t tanh_pair(uint64_t t, uint64_t& u) {
+  u = fmul2(t, t);
+  uint64_t r = ffma2(u, pack2(-0.03377828374505043f, -0.03377828374505043f), pack2(0.1257709264755249f, 0.1257709264755249f));
+  r = ffma2(r, u, pack2(-0.3322276473045349f, -0.3322276473045349f));
+  r = ffma2(r, u, pack2(0.9999555945396423f, 0.9999555945396423f));
   return fmul2(r, t);
+}
+constexpr float kTanhRange2 = 0.5625f;  // square of the range
+__device__ __forceinline__ float fmax3(float a, float b, float c) {
+  float d;
+  asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
+  return d;
 }
 // Four lanes with four 16-byte pieces of a row each: lane c of them gets piece c of all four rows, so that a store of the warp
 // touches 8 rows with 64 bytes each and not 32 with 16.
@@ -454,7 +460,8 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       const int32_t hi_least = __reduce_min_sync(0xffffffffu, there ? keys.hi : 0x7fffffff);
       const int32_t blk0 = e.blk0 + walk.block0(p), n = walk.blocks(p);
       const int32_t step = split ? 2 : 1, first = split ? side : 0;
-      float m = sees ? -INFINITY : 0.f, l = 0.f;  // -inf: no reference yet
+      // -inf: no reference yet.  Capped scores need none, unless the cap is beyond what fp32's range has room for.
+      float m = sees && !(CAP && !BIAS && p.cap <= 80.f) ? -INFINITY : 0.f, l = 0.f;
       float own[2] = {0.f, 0.f};  // this half's sums of the last two blocks
       float moved = 1.f;          // 2^(what the reference moved by for the last block)
       bool aborted = false;
@@ -472,37 +479,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
         tc_fence_after_sync();
         const int32_t b0 = (blk0 + n - 1 - i) * BK, j0 = b0 + half * 64;  // the block's first key, this thread's
         const bool all_begun = b0 >= lo_most, none_ended = b0 + BK <= hi_least;  // what masks may be left out
-        // scores of columns c0.. in log2 units but for a factor (`scale`), -inf where the row does not see the key
-        const float scale = BIAS ? 1.f : CAP ? p.cap : p.scale;
-        auto scores = [&](int c0, uint32_t (&s)[16]) {
-          if (CAP) {
-            uint64_t t[8];
-            float most = 0.f;
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-              t[x] = fmul2(pack2(__uint_as_float(s[2 * x]), __uint_as_float(s[2 * x + 1])), pack2(p.scale, p.scale));
-              float t0, t1;
-              unpack2(t[x], t0, t1);
-              most = fmaxf(most, fmaxf(fabsf(t0), fabsf(t1)));
-            }
-#pragma unroll
-            for (int x = 0; x < 8; ++x) {
-              float t0, t1;
-              unpack2(most <= 1.f ? tanh_pair(t[x]) : t[x], t0, t1);
-              s[2 * x] = __float_as_uint(t0);
-              s[2 * x + 1] = __float_as_uint(t1);
-            }
-            if (!(most <= 1.f)) {  // a row's own way, whatever the others take
-#pragma unroll
-              for (int x = 0; x < 16; ++x) s[x] = __float_as_uint(tanh_fast(__uint_as_float(s[x])));
-            }
-          }
-          if (BIAS) {
-            const float away = (float)(keys.pos - j0 - c0), factor = CAP ? p.cap : p.scale;
-#pragma unroll
-            for (int x = 0; x < 16; ++x)
-              s[x] = __float_as_uint(fmaf(-slope, fabsf(away - (float)x), __uint_as_float(s[x]) * factor));
-          }
+        auto mask = [&](int c0, uint32_t (&s)[16]) {
           if (!all_begun) {
             const int32_t lo = keys.lo - j0 - c0;
 #pragma unroll
@@ -516,6 +493,41 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
               if (x >= hi) s[x] = 0xff800000u;
           }
         };
+        // scores of columns c0.. in log2 units but for a factor (`scale`), -inf where the row does not see the key
+        const float scale = BIAS ? 1.f : CAP ? p.cap : p.scale;
+        auto scores = [&](int c0, uint32_t (&s)[16]) {
+          if (CAP) {
+            float most = 0.f;
+#pragma unroll
+            for (int x = 0; x < 16; x += 2) {
+              uint64_t u;
+              float t0, t1, u0, u1;
+              unpack2(tanh_pair(fmul2(pack2(__uint_as_float(s[x]), __uint_as_float(s[x + 1])), pack2(p.scale, p.scale)), u), t0, t1);
+              unpack2(u, u0, u1);
+              most = fmax3(most, u0, u1);
+              s[x] = __float_as_uint(t0);
+              s[x + 1] = __float_as_uint(t1);
+            }
+            const bool beyond = !(most <= kTanhRange2);
+            if (__any_sync(0xffffffffu, beyond)) {  // rows with a score beyond the polynomial's range: from S again
+              uint32_t again[16];
+              tmem_ld_32x32b_x16(t_s + c0, again);
+              tmem_ld_wait();
+#pragma unroll
+              for (int x = 0; x < 16; ++x) {
+                const float t = tanh_fast(__uint_as_float(again[x]) * p.scale);
+                if (beyond) s[x] = __float_as_uint(t);  // (a row's own way, whatever the others take)
+              }
+            }
+          }
+          if (BIAS) {
+            const float away = (float)(keys.pos - j0 - c0), factor = CAP ? p.cap : p.scale;
+#pragma unroll
+            for (int x = 0; x < 16; ++x)
+              s[x] = __float_as_uint(fmaf(-slope, fabsf(away - (float)x), __uint_as_float(s[x]) * factor));
+          }
+          mask(c0, s);
+        };
         if (slow) {
           if (__any_sync(0xffffffffu, m == -INFINITY)) {  // rows without a reference: the maximum of this block
             float mx = -INFINITY;
@@ -524,13 +536,14 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
               uint32_t s[16];
               tmem_ld_32x32b_x16(t_s + c, s);
               tmem_ld_wait();
-              scores(c, s);
+              if (BIAS) scores(c, s); else mask(c, s);
 #pragma unroll
               for (int x = 0; x < 16; ++x) mx = fmaxf(mx, __uint_as_float(s[x]));
             }
-            *max_own = mx * scale;
+            if (!BIAS) mx = !CAP ? mx * scale : mx == -INFINITY ? mx : scale * tanh_fast(mx * p.scale);  // (a cap keeps the order)
+            *max_own = mx;
             if (!meet(false)) { aborted = true; break; }
-            if (m == -INFINITY) m = fmaxf(mx * scale, *max_other);
+            if (m == -INFINITY) m = fmaxf(mx, *max_other);
           }
           if (__any_sync(0xffffffffu, up != 0.f)) {
             const float a = __uint_as_float((uint32_t)max(127 - (int32_t)up, 0) << 23);  // 2^-up
