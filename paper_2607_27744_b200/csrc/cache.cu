@@ -78,24 +78,29 @@ __device__ __forceinline__ int32_t block_prefix(int32_t v, int32_t& total) {
   return incl - v + (warp > 0 ? base : 0);
 }
 
-// Which index of the call names each slot; kBadSlot in *status where one is out of range or named twice.
-__device__ void claim_slots(const CacheBooks& c, const int32_t* slots, int32_t n, int32_t* owner, int32_t* status) {
-  for (int32_t i = threadIdx.x; i < n; i += kBookThreads) {
-    const int32_t s = slots ? slots[i] : i;
-    if (s < 0 || s >= c.n_slots) atomicMax(status, kBadSlot);
-    else owner[s] = -1;
+// A bit per slot in shared memory for as many slots as fit, otherwise a word per slot in the workspace.
+constexpr int32_t kBitSlots = 32 * 8192;
+struct Claims {
+  uint32_t* bits;  // null: by `owner`
+  int32_t* owner;
+};
+// Clears what claim() uses; a barrier follows.
+__device__ __forceinline__ void clear_claims(const CacheBooks& c, const Claims& k, const int32_t* slots, int32_t n) {
+  if (k.bits) {
+    for (int32_t x = threadIdx.x; x < (c.n_slots + 31) / 32; x += kBookThreads) k.bits[x] = 0;
+  } else {
+    for (int32_t i = threadIdx.x; i < n; i += kBookThreads) {
+      const int32_t s = slots ? slots[i] : i;
+      if (s >= 0 && s < c.n_slots) k.owner[s] = 0;
+    }
   }
   __syncthreads();
-  for (int32_t i = threadIdx.x; i < n; i += kBookThreads) {
-    const int32_t s = slots ? slots[i] : i;
-    if (s >= 0 && s < c.n_slots) atomicMax(owner + s, i);
-  }
-  __syncthreads();
-  for (int32_t i = threadIdx.x; i < n; i += kBookThreads) {
-    const int32_t s = slots ? slots[i] : i;
-    if (s >= 0 && s < c.n_slots && atomicAdd(owner + s, 0) != i) atomicMax(status, kBadSlot);
-  }
-  __syncthreads();
+}
+// false: the slot is none, or has been named by the call already.
+__device__ __forceinline__ bool claim(const CacheBooks& c, const Claims& k, int32_t s) {
+  if (s < 0 || s >= c.n_slots) return false;
+  if (k.bits) return (atomicOr(k.bits + s / 32, 1u << (s % 32)) >> (s % 32) & 1u) == 0;
+  return atomicExch(k.owner + s, 1) == 0;
 }
 
 // The index whose entries entry f is among: largest i with before[i] <= f.
@@ -119,23 +124,36 @@ __device__ __forceinline__ int32_t load_flags(const int32_t* refs, int32_t n_pag
   return m;
 }
 
+constexpr int32_t kNearPages = 4 * kBookThreads;  // free pages that are kept in shared memory
+
 __global__ void __launch_bounds__(kBookThreads, 1)
 extend_kernel(CacheBooks c, const int32_t* slots, const int32_t* off, int32_t R, Books b, int32_t* first, int32_t* report) {
-  __shared__ int32_t status, copies;
+  extern __shared__ uint32_t bits[];
+  __shared__ int32_t status, copies, near_before[kBookThreads + 1], near_place[kBookThreads], near_free[kNearPages];
+  const Claims claims{c.n_slots <= kBitSlots ? bits : nullptr, b.owner};
+  const bool near = R <= kBookThreads;  // the requests' places are kept in shared memory
   if (threadIdx.x == 0) { status = kOk; copies = 0; }
-  __syncthreads();
   ptx::griddep_wait_for(slots, off);
   ptx::griddep_launch_dependents();
-  claim_slots(c, slots, R, b.owner, &status);
+  // the first pages' holders, long before they are asked for
+  int32_t v[4], m = load_flags(c.refs, c.n_pages, 4 * (int32_t)threadIdx.x, v);
+  clear_claims(c, claims, slots, R);
   // pages that each request needs
   int64_t total64 = 0;
+  int32_t my_slot = 0, my_n = 0, my_L = 0, my_start = 0;  // of the last request that this thread looked at
   for (int32_t r0 = 0; r0 < R; r0 += kBookThreads) {
     const int32_t r = r0 + (int32_t)threadIdx.x;
     int32_t need = 0;
     if (r < R) {
       const int32_t s = slots ? slots[r] : r, n = off[r + 1] - off[r];
+      my_slot = s;
+      my_n = n;
+      if (!claim(c, claims, s)) {
+        atomicMax(&status, kBadSlot);
+      }
       if (s >= 0 && s < c.n_slots) {
         const int32_t L = c.lens[s];
+        my_L = L;
         if (L < 0 || (int64_t)L + n > (int64_t)c.width * c.page) {
           atomicMax(&status, kTooLong);
         } else if (n > 0) {
@@ -145,32 +163,40 @@ extend_kernel(CacheBooks c, const int32_t* slots, const int32_t* off, int32_t R,
             if (id < 0 || id >= c.n_pages) atomicMax(&status, kBadPage);
             else copy = c.refs[id] > 1;
           }
-          b.start[r] = pages_for(L, c.page) - (copy ? 1 : 0);
-          need = pages_for(L + n, c.page) - b.start[r];
+          my_start = pages_for(L, c.page) - (copy ? 1 : 0);
+          need = pages_for(L + n, c.page) - my_start;
         } else {
-          b.start[r] = pages_for(L, c.page);
+          my_start = pages_for(L, c.page);
         }
       }
     }
     int32_t sum;
     const int32_t at = block_prefix(need, sum);
-    if (r < R) b.before[r] = (int32_t)total64 + at;
+    if (r < R) {
+      if (near) {
+        near_before[r] = (int32_t)total64 + at;
+        near_place[r] = my_start;
+      } else {
+        b.before[r] = (int32_t)total64 + at;
+        b.start[r] = my_start;
+      }
+    }
     total64 += sum;
     if (total64 > c.n_pages) total64 = (int64_t)c.n_pages + 1;  // more than there are, whatever comes: refused below
   }
   const int32_t total = (int32_t)total64;
-  if (threadIdx.x == 0) b.before[R] = total;
   // that many free pages, lowest first
   int32_t found = 0;
   for (int32_t p0 = 0; p0 < c.n_pages && found < total; p0 += 4 * kBookThreads) {
-    int32_t v[4];
-    const int32_t p = p0 + 4 * (int32_t)threadIdx.x, m = load_flags(c.refs, c.n_pages, p, v);
+    const int32_t p = p0 + 4 * (int32_t)threadIdx.x;
+    if (p0 > 0) m = load_flags(c.refs, c.n_pages, p, v);
     int32_t mine = 0, sum;
     for (int k = 0; k < 4; ++k) mine += k < m && v[k] == 0;
     int32_t at = found + block_prefix(mine, sum);
     for (int k = 0; k < 4; ++k)
       if (k < m && v[k] == 0) {
-        if (at < total) b.map[at] = p + k;
+        if (at < kNearPages) near_free[at] = p + k;
+        else if (at < total) b.map[at] = p + k;
         ++at;
       }
     found += sum;
@@ -191,23 +217,31 @@ extend_kernel(CacheBooks c, const int32_t* slots, const int32_t* off, int32_t R,
     if (threadIdx.x == 0) b.head[2] = 0;
     return;
   }
+  const int32_t* before = near ? near_before : b.before;
+  const int32_t* place = near ? near_place : b.start;
+  auto free_page = [&](int32_t f) { return f < kNearPages ? near_free[f] : b.map[f]; };
   // shared last pages: from there the row is a copy's; their entries are still the old ones
   for (int32_t r = threadIdx.x; r < R; r += kBookThreads) {
-    const int32_t s = slots ? slots[r] : r, n = off[r + 1] - off[r], L = c.lens[s];
-    first[r] = L;
-    if (n > 0 && b.start[r] < pages_for(L, c.page)) {
-      const int32_t id = c.table[(int64_t)s * c.width + b.start[r]], at = atomicAdd(&copies, 1);
+    if (!near) {
+      my_slot = slots ? slots[r] : r;
+      my_n = off[r + 1] - off[r];
+      my_L = c.lens[my_slot];
+      my_start = place[r];
+    }
+    first[r] = my_L;
+    if (my_n > 0 && my_start < pages_for(my_L, c.page)) {
+      const int32_t id = c.table[(int64_t)my_slot * c.width + my_start], at = atomicAdd(&copies, 1);
       b.src[at] = id;
-      b.dst[at] = b.map[b.before[r]];
+      b.dst[at] = free_page(before[r]);
       atomicSub(c.refs + id, 1);
     }
-    c.lens[s] = L + n;
+    c.lens[my_slot] = my_L + my_n;
   }
   __syncthreads();
   if (threadIdx.x == 0) b.head[2] = copies;
   for (int32_t f = threadIdx.x; f < total; f += kBookThreads) {
-    const int32_t r = index_of(b.before, R, f), s = slots ? slots[r] : r, id = b.map[f];
-    c.table[(int64_t)s * c.width + b.start[r] + (f - b.before[r])] = id;
+    const int32_t r = index_of(before, R, f), s = slots ? slots[r] : r, id = free_page(f);
+    c.table[(int64_t)s * c.width + place[r] + (f - before[r])] = id;
     c.refs[id] = 1;
   }
 }
@@ -235,18 +269,25 @@ __device__ void apply_truncate(const CacheBooks& c, const int32_t* slots, int32_
 __global__ void __launch_bounds__(kBookThreads, 1)
 check_kernel(CacheBooks c, const int32_t* parents, const int32_t* slots, const int32_t* keep, int32_t n, Books b, int32_t* report,
              bool carry_out) {
-  __shared__ int32_t status;
+  extern __shared__ uint32_t bits[];
+  __shared__ int32_t status, near_before[kBookThreads + 1], near_place[kBookThreads];
+  const Claims claims{c.n_slots <= kBitSlots ? bits : nullptr, b.owner};
+  const bool near = carry_out && n <= kBookThreads;  // the slots' places are kept in shared memory
+  if (near) {
+    b.before = near_before;
+    b.start = near_place;
+  }
   if (threadIdx.x == 0) status = kOk;
-  __syncthreads();
   ptx::griddep_wait_for(parents, slots, keep);
   ptx::griddep_launch_dependents();
-  claim_slots(c, slots, n, b.owner, &status);
+  clear_claims(c, claims, slots, n);
   int64_t total64 = 0;
   for (int32_t i0 = 0; i0 < n; i0 += kBookThreads) {
     const int32_t i = i0 + (int32_t)threadIdx.x;
     int32_t entries = 0;
     if (i < n) {
       const int32_t s = slots[i];
+      if (!claim(c, claims, s)) atomicMax(&status, kBadSlot);
       if (s >= 0 && s < c.n_slots) {
         const int32_t L = c.lens[s];
         if (parents) {
@@ -414,6 +455,7 @@ __global__ void __launch_bounds__(kCopyThreads) copy_pages_kernel(PageShape g, C
 }
 
 // A warp per new row.
+constexpr int kAhead = 4;  // 16-byte vectors of K and of V per lane
 struct AppendArgs {
   CacheBooks c;
   const int32_t *slots, *off, *first;
@@ -425,26 +467,58 @@ struct AppendArgs {
   const uint8_t *K_new, *V_new;
   int64_t new_token_bytes, new_head_bytes;
 };
+// The request that row i of the batch is of, found by a warp: 32 offsets at a time.
+__device__ __forceinline__ int32_t request_of(const int32_t* off, int32_t R, int64_t i, int lane) {
+  int32_t lo = 0, n = R;  // requests lo .. lo + n - 1 may have the row
+  while (n > 1) {
+    const int32_t step = (n + 31) / 32, at = lo + lane * step;
+    const uint32_t begun = __ballot_sync(0xffffffffu, lane * step < n && off[at] <= i);  // (the first has)
+    const int32_t last = 31 - __clz((int)begun);
+    n = min(step, n - last * step);
+    lo += last * step;
+  }
+  return lo;
+}
+
 __global__ void __launch_bounds__(256) append_kernel(AppendArgs a) {
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const int lane = threadIdx.x % 32;
+  const int32_t total = a.H_kv * a.vecs;
   for (int64_t i = (int64_t)blockIdx.x * 8 + threadIdx.x / 32; i < a.N; i += (int64_t)gridDim.x * 8) {
-    const int32_t r = RequestMap{nullptr, a.off, a.R}.of(i);
+    // the row's values are on their way while its place is looked up
+    const int64_t from = i * a.new_token_bytes;
+    uint4 k[kAhead], v[kAhead];
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const int32_t e = lane + 32 * x, h = e / a.vecs, at = (e - h * a.vecs) * 16;
+      if (e < total) {
+        k[x] = *reinterpret_cast<const uint4*>(a.K_new + from + h * a.new_head_bytes + at);
+        v[x] = *reinterpret_cast<const uint4*>(a.V_new + from + h * a.new_head_bytes + at);
+      }
+    }
+    const int32_t r = request_of(a.off, a.R, i, lane);
     const int32_t s = a.slots ? a.slots[r] : r, first = a.first[r];
     if (s < 0 || s >= a.c.n_slots || first < 0) continue;
     const int64_t pos = (int64_t)first + (i - a.off[r]);
     if (pos >= (int64_t)a.c.width * a.c.page) continue;
     const int32_t id = a.c.table[(int64_t)s * a.c.width + (int32_t)pos / a.c.page];
     if (id < 0 || id >= a.c.n_pages) continue;
-    const int64_t to = id * a.page_bytes + ((int32_t)pos % a.c.page) * a.token_bytes, from = i * a.new_token_bytes;
-    const int32_t total = a.H_kv * a.vecs;
-    for (int32_t e = lane; e < total; e += 32) {
-      const int32_t h = e / a.vecs, x = (e - h * a.vecs) * 16;
-      const uint4 k = *reinterpret_cast<const uint4*>(a.K_new + from + h * a.new_head_bytes + x);
-      const uint4 v = *reinterpret_cast<const uint4*>(a.V_new + from + h * a.new_head_bytes + x);
-      *reinterpret_cast<uint4*>(a.K + to + h * a.head_bytes + x) = k;
-      *reinterpret_cast<uint4*>(a.V + to + h * a.head_bytes + x) = v;
+    const int64_t to = id * a.page_bytes + ((int32_t)pos % a.c.page) * a.token_bytes;
+#pragma unroll
+    for (int x = 0; x < kAhead; ++x) {
+      const int32_t e = lane + 32 * x, h = e / a.vecs, at = (e - h * a.vecs) * 16;
+      if (e < total) {
+        *reinterpret_cast<uint4*>(a.K + to + h * a.head_bytes + at) = k[x];
+        *reinterpret_cast<uint4*>(a.V + to + h * a.head_bytes + at) = v[x];
+      }
+    }
+    for (int32_t e = lane + 32 * kAhead; e < total; e += 32) {
+      const int32_t h = e / a.vecs, at = (e - h * a.vecs) * 16;
+      const uint4 kx = *reinterpret_cast<const uint4*>(a.K_new + from + h * a.new_head_bytes + at);
+      const uint4 vx = *reinterpret_cast<const uint4*>(a.V_new + from + h * a.new_head_bytes + at);
+      *reinterpret_cast<uint4*>(a.K + to + h * a.head_bytes + at) = kx;
+      *reinterpret_cast<uint4*>(a.V + to + h * a.head_bytes + at) = vx;
     }
   }
 }
@@ -489,6 +563,8 @@ rocs_status_t check_books(const rocs_cache* c, int32_t n, const void* workspace,
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || bytes < rocs_cache_workspace(c, n)) return ROCS_ERR_WORKSPACE;
   return ROCS_OK;
 }
+
+size_t claim_bytes(const rocs_cache* c) { return c->n_slots <= kBitSlots ? sizeof(uint32_t) * (size_t)((c->n_slots + 31) / 32) : 0; }
 
 // How many CTAs copy: a few per SM of the chip, fewer where the pool could not give them a piece each.
 unsigned copy_grid(const rocs_cache* c, const PageShape& g, int64_t most_pairs, int64_t entries) {
@@ -557,7 +633,8 @@ rocs_status_t rocs_cache_extend(const rocs_cache_t* c, const rocs_plan_t* plan, 
   if (st != ROCS_OK) return st;
   cudaStream_t stream = (cudaStream_t)stream_;
   const Books b = books_in(workspace, c, plan->R);
-  const rocs_status_t launched = launch_dependent(extend_kernel, dim3(1), kBookThreads, 0, stream, books_of(c), slots,
+  ROCS_ALLOW_SMEM(extend_kernel, kBitSlots / 8);
+  const rocs_status_t launched = launch_dependent(extend_kernel, dim3(1), kBookThreads, claim_bytes(c), stream, books_of(c), slots,
                                                   plan->cand_offsets, plan->R, b, first, report);
   if (launched != ROCS_OK) return launched;
   const PageShape g = page_shape(c);
@@ -572,8 +649,9 @@ static rocs_status_t fork_or_truncate(const rocs_cache_t* c, int32_t n, const in
   const Books b = books_in(workspace, c, n);
   const int64_t most = (int64_t)n * c->width;
   const bool one = most <= kOneCtaEntries;
+  ROCS_ALLOW_SMEM(check_kernel, kBitSlots / 8);
   const rocs_status_t launched =
-      launch_dependent(check_kernel, dim3(1), kBookThreads, 0, stream, books_of(c), parents, slots, keep, n, b, report, one);
+      launch_dependent(check_kernel, dim3(1), kBookThreads, claim_bytes(c), stream, books_of(c), parents, slots, keep, n, b, report, one);
   if (launched != ROCS_OK || one) return launched;
   return launch_dependent(apply_kernel, dim3((unsigned)std::min<int64_t>((most + 255) / 256, 4 * (int64_t)sm_count())), 256, 0, stream,
                           books_of(c), parents, slots, n, b);
