@@ -523,12 +523,6 @@ __global__ void __launch_bounds__(256) append_kernel(AppendArgs a) {
   }
 }
 
-int sm_count() {
-  int dev = 0, n = 148;
-  if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-  return n;
-}
-
 PageShape page_shape(const rocs_cache* c) {
   const int64_t es = (int64_t)elem_size(c->dtype);
   PageShape g{};
@@ -570,7 +564,7 @@ size_t claim_bytes(const rocs_cache* c) { return c->n_slots <= kBitSlots ? sizeo
 unsigned copy_grid(const rocs_cache* c, const PageShape& g, int64_t most_pairs, int64_t entries) {
   const int64_t chunks = ((int64_t)g.outer * g.inner * g.vecs + kChunk - 1) / kChunk;
   const int64_t want = std::max(most_pairs * c->layers * 2 * chunks, (entries + kCopyThreads - 1) / kCopyThreads);
-  return (unsigned)std::max<int64_t>(1, std::min<int64_t>(want, 4 * (int64_t)sm_count()));
+  return (unsigned)std::max<int64_t>(1, std::min<int64_t>(want, 4 * (int64_t)sms_of_device()));
 }
 
 }  // namespace
@@ -653,7 +647,7 @@ static rocs_status_t fork_or_truncate(const rocs_cache_t* c, int32_t n, const in
   const rocs_status_t launched =
       launch_dependent(check_kernel, dim3(1), kBookThreads, claim_bytes(c), stream, books_of(c), parents, slots, keep, n, b, report, one);
   if (launched != ROCS_OK || one) return launched;
-  return launch_dependent(apply_kernel, dim3((unsigned)std::min<int64_t>((most + 255) / 256, 4 * (int64_t)sm_count())), 256, 0, stream,
+  return launch_dependent(apply_kernel, dim3((unsigned)std::min<int64_t>((most + 255) / 256, 4 * (int64_t)sms_of_device())), 256, 0, stream,
                           books_of(c), parents, slots, n, b);
 }
 
@@ -713,7 +707,7 @@ rocs_status_t rocs_cache_append(const rocs_cache_t* c, int32_t layer, const rocs
   a.new_token_bytes = ld_token * es;
   a.new_head_bytes = ld_head * es;
   const int64_t ctas = (plan->N + 7) / 8;
-  return launch_dependent(append_kernel, dim3((unsigned)std::min<int64_t>(ctas, 16 * (int64_t)sm_count())), 256, 0,
+  return launch_dependent(append_kernel, dim3((unsigned)std::min<int64_t>(ctas, 16 * (int64_t)sms_of_device())), 256, 0,
                           (cudaStream_t)stream, a);
 }
 

@@ -17,6 +17,17 @@ namespace rocs {
 
 int kernel_path();  // of rocs_set_path
 
+// SMs of the current device, asked for once per device.
+inline int sms_of_device() {
+  static std::atomic<int> known[64];
+  int dev = 0, n = 148;
+  if (cudaGetDevice(&dev) != cudaSuccess) return n;
+  if (dev < 64 && (n = known[dev].load(std::memory_order_relaxed)) != 0) return n;
+  if (cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev) != cudaSuccess) return 148;
+  if (dev < 64) known[dev].store(n, std::memory_order_relaxed);
+  return n;
+}
+
 #ifdef __CUDACC__
 __device__ __forceinline__ int32_t pages_for(int32_t positions, int32_t page) { return (positions + page - 1) / page; }
 #endif

@@ -329,12 +329,6 @@ rocs_status_t general_of(const CacheAttn& p, int32_t grid, cudaStream_t stream) 
   return launch_general<T, 8>(p, grid, stream);
 }
 
-int sm_count() {
-  int dev = 0, n = 148;
-  if (cudaGetDevice(&dev) == cudaSuccess) cudaDeviceGetAttribute(&n, cudaDevAttrMultiProcessorCount, dev);
-  return n;
-}
-
 enum class Kind { kGeneral, kMma, kFew, kUmma };
 
 // Which kernel a call takes, and how its work is cut.
@@ -345,15 +339,15 @@ struct Choice {
   int64_t entries;
   bool by_request;  // no request has more than one tile
 };
-Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H) {
+Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H, int path) {
   Choice x{};
-  const int32_t g = H / c->H_kv, sms = sm_count();
+  const int32_t g = H / c->H_kv, sms = sms_of_device();
   int32_t most = 16;
   x.kind = Kind::kGeneral;
   x.block = kGenKeys;
   x.min_units = 2;
   x.extra = 1;
-  if (c->dtype == ROCS_BF16 && kernel_path() == ROCS_PATH_AUTO && (c->dh == 32 || c->dh == 64 || c->dh == 128)) {
+  if (c->dtype == ROCS_BF16 && path == ROCS_PATH_AUTO && (c->dh == 32 || c->dh == 64 || c->dh == 128)) {
     x.kind = Kind::kMma;
     x.block = kMmaKeys;
     if ((int64_t)plan->largest * g > 16) most = 64;
@@ -417,7 +411,9 @@ extern "C" {
 
 size_t rocs_cache_attention_workspace(const rocs_cache_t* c, const rocs_plan_t* plan, int32_t H) {
   if (!c || !plan || H < 1 || H % c->H_kv != 0) return 0;
-  return places(choose(c, plan, H), c->dh).bytes;
+  size_t most = 0;  // whichever path is in force when it is used
+  for (int path : {ROCS_PATH_AUTO, ROCS_PATH_GENERAL}) most = std::max(most, places(choose(c, plan, H, path), c->dh).bytes);
+  return most;
 }
 
 rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const rocs_plan_t* plan, const int32_t* slots, int32_t H,
@@ -433,7 +429,7 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
   if ((H > 1 && ld_oh < c->dh) || (plan->N > 1 && ld_ot < c->dh)) return ROCS_ERR_INVALID_ARG;  // rows of O share no memory
   if (H > 65535) return ROCS_ERR_UNSUPPORTED;
   if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)c->dh);
-  const Choice x = choose(c, plan, H);
+  const Choice x = choose(c, plan, H, kernel_path());
   const Places w = places(x, c->dh);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || bytes < w.bytes) return ROCS_ERR_WORKSPACE;
   if (x.entries > 0x7fffffffLL) return ROCS_ERR_UNSUPPORTED;
