@@ -122,7 +122,9 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(CacheAttn p, int32_t
 
 template <typename T>
 rocs_status_t join_parts(const CacheAttn& p, int32_t rows, int32_t grid, cudaStream_t stream) {
-  const dim3 blocks((unsigned)grid, (unsigned)std::min((rows + 3) / 4, 32));
+  // with as many tiles as CTAs few are cut, and most blocks have nothing to do; with fewer all are, into many parts
+  const int most = (int64_t)p.entries * p.heads >= grid ? 16 : 64;
+  const dim3 blocks((unsigned)grid, (unsigned)std::min((rows + 3) / 4, most));
   if (p.dh <= 64) return launch_dependent(join_kernel<T, 2>, blocks, kJoinThreads, 0, stream, p, grid);
   if (p.dh <= 128) return launch_dependent(join_kernel<T, 4>, blocks, kJoinThreads, 0, stream, p, grid);
   return launch_dependent(join_kernel<T, 8>, blocks, kJoinThreads, 0, stream, p, grid);
@@ -335,7 +337,7 @@ enum class Kind { kGeneral, kMma, kFew, kUmma };
 struct Choice {
   Kind kind;
   int32_t group, per_kv, heads;  // query heads per tile row, such groups per key head, groups in all
-  int32_t rows_per_tile, tile_rows, block, min_units, extra, grid;
+  int32_t rows_per_tile, tile_rows, block, min_shift, extra, grid;
   int64_t entries;
   bool by_request;  // no request has more than one tile
 };
@@ -345,7 +347,7 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H, int path) {
   int32_t most = 16;
   x.kind = Kind::kGeneral;
   x.block = kGenKeys;
-  x.min_units = 2;
+  x.min_shift = 1;
   x.extra = 1;
   if (c->dtype == ROCS_BF16 && path == ROCS_PATH_AUTO && (c->dh == 32 || c->dh == 64 || c->dh == 128)) {
     x.kind = Kind::kMma;
@@ -354,12 +356,20 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H, int path) {
     else if (attn_few_supported(c->dh, c->page)) {
       x.kind = Kind::kFew;
       x.block = kFewKeys;
+      x.extra = 1;
+      x.min_shift = 1;
       if ((int64_t)plan->largest * g <= 8) most = 8;
     }
-    if ((int64_t)plan->largest * g > 64 && attn_umma_supported(c->dh, c->page)) {
+    // Few rows: a tile of the tcgen05 kernel takes about 6 us beside its keys, one of the other kernel 2 us and longer for each
+    // key.  Rows of each of 6 requests over 250 keys, 4 heads of 64, tcgen05 and the other: 20 / 40 / 64 / 100 / 148 rows 18.0 /
+    // 18.8 / 20.2 / 21.8 / 20.0 and 12.2 / 14.2 / 17.2 / 18.6 / 18.7 us; 24 requests over 1000 keys, 8 heads of 64: 40 / 64 / 100
+    // rows 28.3 / 28.7 / 29.8 and 28.7 / 32.3 / 47.9; 8 over 2000, 8 heads of 128: 40 / 64 / 100 rows 26.9 / 27.9 / 30.2 and 34.8 /
+    // 37.6 / 58.8.  How many keys there are is known on the device only; the table's width says how many there may be.
+    const bool many_keys = (int64_t)c->width * c->page >= 512;
+    if ((int64_t)plan->largest * g > (many_keys ? 32 : 128) && attn_umma_supported(c->dh, c->page)) {
       x.kind = Kind::kUmma;
       x.block = kUmmaKeys;
-      x.min_units = 8;
+      x.min_shift = 3;
       x.extra = 4;
       most = 128;  // of a side
     }
@@ -473,10 +483,9 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
   p.cap = cap * to_unit;
   p.slopes = slopes;
   p.block = x.block;
-  p.min_units = x.min_units;
+  p.min_shift = x.min_shift;
   p.extra = x.extra;
   p.light_rows = x.kind == Kind::kUmma ? x.rows_per_tile / 2 : x.rows_per_tile;
-  p.heavy = 2;
   p.tile_rows = x.tile_rows;
   uint8_t* ws = static_cast<uint8_t*>(workspace);
   p.meta = reinterpret_cast<AttnMeta*>(ws + w.meta);

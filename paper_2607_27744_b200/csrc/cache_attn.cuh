@@ -54,9 +54,9 @@ struct CacheAttn {
   // scores in units of 1 / unit powers of two: scale * log2(e) / unit; capped: scale / cap, then cap * log2(e) / unit
   float scale, cap, unit;
   const float* slopes;
-  int32_t block, min_units; // keys of a block, least units of a CTA
+  int32_t block, min_shift; // keys of a block, least units of a CTA (2^)
   int32_t extra;            // units of a tile beside its blocks'
-  int32_t light_rows, heavy;  // a block weighs 1 in a tile of up to so many batch rows, otherwise `heavy`
+  int32_t light_rows;       // a block weighs 1 in a tile of up to so many batch rows, otherwise 2
   int32_t tile_rows;        // rows of a tile as the parts hold them (batch rows x group, rounded up)
   // workspace
   int64_t* line_global;     // [entries + 1]
@@ -126,7 +126,7 @@ __device__ __forceinline__ void attn_blocks(const CacheAttn& p, AttnEntry& e, in
   e.blocks = last > first_key ? (last + p.block - 1) / p.block - e.blk0 : 0;
 }
 // Units of a tile: `extra` for its beginning and end, and a block's weight for each block.
-__device__ __forceinline__ int32_t attn_weight(const CacheAttn& p, const AttnEntry& e) { return e.count > p.light_rows ? p.heavy : 1; }
+__device__ __forceinline__ int32_t attn_weight(const CacheAttn& p, const AttnEntry& e) { return e.count > p.light_rows ? 2 : 1; }
 __device__ __forceinline__ uint32_t attn_cost(const CacheAttn& p, const AttnEntry& e) {
   return e.count > 0 ? (uint32_t)(p.extra + max(e.blocks, 1) * attn_weight(p, e)) : 0u;
 }
@@ -192,26 +192,39 @@ struct AttnWalk {
   __device__ __forceinline__ static int64_t over(int64_t x, int32_t d) {
     return x >> 32 == 0 ? (int64_t)((uint32_t)x / (uint32_t)d) : x / d;
   }
-  // The tile that unit x < total is in, and x moved down to where a piece may begin: the tile's first unit, or a block.
+  // The tile that unit x < total is in, and x moved down to where a piece may begin: the tile's first unit, or a block.  All
+  // lanes of a warp call it: a line in shared memory is looked through 32 tiles at a time.
   __device__ __forceinline__ int64_t find(const CacheAttn& p, const AttnLineView& v, int64_t x) {
-    int32_t lo = 0, hi = p.entries;  // largest entry that begins at or before x
-    while (hi - lo > 1) {
-      const int32_t mid = lo + (hi - lo) / 2;
-      if (v.line[mid] * p.heads <= x) lo = mid; else hi = mid;
+    const int64_t of_heads = over(x, p.heads);  // an entry begins at or before x where its line does at or before this
+    int32_t lo = 0;                             // largest such entry
+    if (p.listed) {
+      int32_t hi = p.entries;
+      while (hi - lo > 1) {
+        const int32_t mid = lo + (hi - lo) / 2;
+        if (v.line[mid] <= of_heads) lo = mid; else hi = mid;
+      }
+    } else {
+      int32_t begun = 0;
+      for (int32_t i0 = 0; i0 < p.entries; i0 += 32) {
+        const int32_t i = i0 + (int32_t)(threadIdx.x % 32);
+        begun += __popc(__ballot_sync(0xffffffffu, i < p.entries && v.line[i] <= of_heads));
+      }
+      lo = begun - 1;
     }
     entry = lo;
-    cost = (int32_t)(v.line[lo + 1] - v.line[lo]);
-    head = (int32_t)over(x - v.line[lo] * p.heads, cost);
-    tile_begin = v.line[lo] * p.heads + (int64_t)head * cost;
+    const int64_t begin = v.line[lo];
+    cost = (int32_t)(v.line[lo + 1] - begin);
+    head = (int32_t)over(x - begin * p.heads, cost);
+    tile_begin = begin * p.heads + (int64_t)head * cost;
     weight = attn_weight(p, v.entry[lo]);
-    const int32_t block = ((int32_t)(x - tile_begin) - p.extra) / weight;
+    const int32_t block = ((int32_t)(x - tile_begin) - p.extra) >> (weight - 1);
     return block <= 0 ? tile_begin : tile_begin + p.extra + block * weight;
   }
   // false: nothing for this CTA.  Its thread NOTER, one that has little else to do, notes what the joining kernel needs.
   template <int NOTER>
   __device__ __forceinline__ bool start(const CacheAttn& p, const AttnLineView& v) {
     const int64_t total = v.line[p.entries] * p.heads;
-    const int32_t ctas = (int32_t)min((int64_t)gridDim.x, max(over(total, p.min_units), (int64_t)1));
+    const int32_t ctas = (int32_t)min((int64_t)gridDim.x, max(total >> p.min_shift, (int64_t)1));
     const int32_t i = blockIdx.x;
     u = end = 0;
     first = true;
@@ -247,10 +260,10 @@ struct AttnWalk {
   }
   __device__ __forceinline__ bool more() const { return u < end; }
   __device__ __forceinline__ int32_t block0(const CacheAttn& p) const {
-    return u == tile_begin ? 0 : ((int32_t)(u - tile_begin) - p.extra) / weight;
+    return u == tile_begin ? 0 : ((int32_t)(u - tile_begin) - p.extra) >> (weight - 1);
   }
   __device__ __forceinline__ int32_t blocks(const CacheAttn& p) const {
-    return ((int32_t)(min(end, tile_begin + cost) - tile_begin) - p.extra) / weight - block0(p);
+    return (((int32_t)(min(end, tile_begin + cost) - tile_begin) - p.extra) >> (weight - 1)) - block0(p);
   }
   __device__ __forceinline__ bool whole() const { return u == tile_begin && end >= tile_begin + cost; }
   // where a part goes: a CTA's first piece to its first place, otherwise (its last) to the second

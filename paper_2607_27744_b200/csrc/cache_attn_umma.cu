@@ -532,13 +532,17 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
           if (__any_sync(0xffffffffu, m == -INFINITY)) {  // rows without a reference: the maximum of this block
             float mx = -INFINITY;
 #pragma unroll 1
-            for (int c = 0; c < 64; c += 16) {
-              uint32_t s[16];
-              tmem_ld_32x32b_x16(t_s + c, s);
+            for (int c = 0; c < 64; c += 32) {
+              uint32_t s[2][16];
+              tmem_ld_32x32b_x16(t_s + c, s[0]);
+              tmem_ld_32x32b_x16(t_s + c + 16, s[1]);
               tmem_ld_wait();
-              if (BIAS) scores(c, s); else mask(c, s);
 #pragma unroll
-              for (int x = 0; x < 16; ++x) mx = fmaxf(mx, __uint_as_float(s[x]));
+              for (int y = 0; y < 2; ++y) {
+                if (BIAS) scores(c + y * 16, s[y]); else mask(c + y * 16, s[y]);
+#pragma unroll
+                for (int x = 0; x < 16; x += 2) mx = fmax3(mx, __uint_as_float(s[y][x]), __uint_as_float(s[y][x + 1]));
+              }
             }
             if (!BIAS) mx = !CAP ? mx * scale : mx == -INFINITY ? mx : scale * tanh_fast(mx * p.scale);  // (a cap keeps the order)
             *max_own = mx;
