@@ -68,24 +68,44 @@ __device__ __forceinline__ void store_row(uint8_t* out, int32_t c, float v) {
 }
 
 // Joins the parts of the tiles that a cut went through: O = sum_i 2^(m_i - M) O_i / sum_i 2^(m_i - M) l_i, part by part in
-// the order of the keys with the largest reference so far as M.  A warp per row, lanes are output columns; blockIdx.x is the
-// cut.  Four parts are fetched at once: the kernel is a few trips to memory long.
-constexpr int kJoinThreads = 128;
+// the order of the keys with the largest reference so far as M.  Lanes are output columns; blockIdx.x is the cut.  A warp per
+// row, or the block's four warps per row where there are more than kFewParts parts (a long sequence over the whole chip: 2
+// rows of 17000 keys, 4 key heads of 64, 55 parts each, 23 us with a warp per row), each with every fourth group of four parts.
+// Four parts are fetched at once: the kernel is a few trips to memory long.
+constexpr int kJoinThreads = 128, kFewParts = 8;
+template <int NV>
+struct Joined {
+  float M = -INFINITY, l = 0.f, acc[NV];
+  __device__ __forceinline__ void add(float m, float sum, const float (&o)[NV], float unit) {
+    // a part in which the row saw no key, or only scores of -inf, adds nothing (its sum is 0, or NaN)
+    if (m == -INFINITY) {
+      l += sum;
+      return;
+    }
+    const float M_new = fmaxf(M, m), a = M == M_new ? 1.f : exp2f((M - M_new) * unit), w = exp2f((m - M_new) * unit);
+    M = M_new;
+    l = fmaf(l, a, w * sum);
+#pragma unroll
+    for (int c = 0; c < NV; ++c) acc[c] = fmaf(acc[c], a, w * o[c]);
+  }
+};
 template <typename T, int NV>
 __global__ void __launch_bounds__(kJoinThreads) join_kernel(CacheAttn p, int32_t grid) {
+  __shared__ float other[3][NV * 32 + 2];
   ptx::griddep_wait();
   ptx::griddep_launch_dependents();
   const AttnMeta m = p.meta[blockIdx.x];
   if (m.parts == 0) return;
   const AttnEntry& e = m.entry;
-  const int lane = threadIdx.x % 32;
+  const int lane = threadIdx.x % 32, warp = threadIdx.x / 32;
   auto place = [&](int32_t i) { return i == 0 ? m.place : 2 * ((int32_t)blockIdx.x - 1 + i); };
-  const int32_t rows = e.count * p.group;
-  for (int32_t row = blockIdx.y * (kJoinThreads / 32) + threadIdx.x / 32; row < rows; row += gridDim.y * (kJoinThreads / 32)) {
-    float M = -INFINITY, l = 0.f, acc[NV];
+  const bool many = m.parts > kFewParts;
+  const int32_t rows = e.count * p.group, row0 = many ? blockIdx.y : blockIdx.y * 4 + warp, row_step = many ? gridDim.y : gridDim.y * 4;
+  for (int32_t row = row0; row < rows; row += row_step) {
+    Joined<NV> sum;
 #pragma unroll
-    for (int c = 0; c < NV; ++c) acc[c] = 0.f;
-    for (int32_t i0 = 0; i0 < m.parts; i0 += 4) {
+    for (int c = 0; c < NV; ++c) sum.acc[c] = 0.f;
+    for (int32_t i0 = many ? warp * 4 : 0; i0 < m.parts; i0 += many ? 16 : 4) {
       float2 s[4];
       float o[4][NV];
 #pragma unroll
@@ -98,33 +118,44 @@ __global__ void __launch_bounds__(kJoinThreads) join_kernel(CacheAttn p, int32_t
         for (int c = 0; c < NV; ++c) o[k][c] = lane + 32 * c < p.dh ? from[lane + 32 * c] : 0.f;
       }
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        // a part in which the row saw no key, or only scores of -inf, adds nothing (its sum is 0, or NaN)
-        if (s[k].x == -INFINITY) {
-          l += s[k].y;
-          continue;
-        }
-        const float M_new = fmaxf(M, s[k].x), a = M == M_new ? 1.f : exp2f((M - M_new) * p.unit), w = exp2f((s[k].x - M_new) * p.unit);
-        M = M_new;
-        l = fmaf(l, a, w * s[k].y);
+      for (int k = 0; k < 4; ++k) sum.add(s[k].x, s[k].y, o[k], p.unit);
+    }
+    if (many) {  // the warps' sums, in order
+      if (warp > 0) {
 #pragma unroll
-        for (int c = 0; c < NV; ++c) acc[c] = fmaf(acc[c], a, w * o[k][c]);
+        for (int c = 0; c < NV; ++c) other[warp - 1][c * 32 + lane] = sum.acc[c];
+        if (lane == 0) {
+          other[warp - 1][NV * 32] = sum.M;
+          other[warp - 1][NV * 32 + 1] = sum.l;
+        }
       }
+      __syncthreads();
+      if (warp == 0)
+        for (int w = 0; w < 3; ++w) {
+          float o[NV];
+#pragma unroll
+          for (int c = 0; c < NV; ++c) o[c] = other[w][c * 32 + lane];
+          sum.add(other[w][NV * 32], other[w][NV * 32 + 1], o, p.unit);
+        }
+      __syncthreads();
+      if (warp > 0) continue;
     }
     const int32_t t = row / p.group;
     const RowKeys keys = attn_row(p, e, t);
     uint8_t* out = p.O + (int64_t)(e.row0 + t) * p.o_row_bytes + (m.head * p.group + row % p.group) * p.o_head_bytes;
 #pragma unroll
     for (int c = 0; c < NV; ++c)
-      if (lane + 32 * c < p.dh) store_row<T>(out, lane + 32 * c, keys.lo < keys.hi ? acc[c] / l : 0.f);
+      if (lane + 32 * c < p.dh) store_row<T>(out, lane + 32 * c, keys.lo < keys.hi ? sum.acc[c] / sum.l : 0.f);
   }
 }
 
 template <typename T>
 rocs_status_t join_parts(const CacheAttn& p, int32_t rows, int32_t grid, cudaStream_t stream) {
-  // with as many tiles as CTAs few are cut, and most blocks have nothing to do; with fewer all are, into many parts
-  const int most = (int64_t)p.entries * p.heads >= grid ? 16 : 64;
-  const dim3 blocks((unsigned)grid, (unsigned)std::min((rows + 3) / 4, most));
+  // with as many tiles as CTAs few are cut; with fewer all are, into many parts.  (Two rounds of blocks at most: those of cuts
+  // that need no joining only look that up.)
+  const bool all_cut = (int64_t)p.entries * p.heads < grid;
+  const int32_t most = std::max(2 * 16 * sms_of_device() / grid, 4);
+  const dim3 blocks((unsigned)grid, (unsigned)std::min(all_cut ? rows : (rows + 3) / 4, most));
   if (p.dh <= 64) return launch_dependent(join_kernel<T, 2>, blocks, kJoinThreads, 0, stream, p, grid);
   if (p.dh <= 128) return launch_dependent(join_kernel<T, 4>, blocks, kJoinThreads, 0, stream, p, grid);
   return launch_dependent(join_kernel<T, 8>, blocks, kJoinThreads, 0, stream, p, grid);
@@ -356,8 +387,8 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H, int path) {
     else if (attn_few_supported(c->dh, c->page)) {
       x.kind = Kind::kFew;
       x.block = kFewKeys;
-      x.extra = 1;
-      x.min_shift = 1;
+      x.extra = 4;
+      x.min_shift = 2;
       if ((int64_t)plan->largest * g <= 8) most = 8;
     }
     // Few rows: a tile of the tcgen05 kernel takes about 6 us beside its keys, one of the other kernel 2 us and longer for each
@@ -369,7 +400,7 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H, int path) {
     if ((int64_t)plan->largest * g > (many_keys ? 32 : 128) && attn_umma_supported(c->dh, c->page)) {
       x.kind = Kind::kUmma;
       x.block = kUmmaKeys;
-      x.min_shift = 3;
+      x.min_shift = 2;
       x.extra = 4;
       most = 128;  // of a side
     }
