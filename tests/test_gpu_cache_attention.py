@@ -316,3 +316,96 @@ def test_all_visible_scores_at_the_lowest_value_and_beyond():
     cache = rocs.cache_create(case["K"], case["V"], case["table"], case["lens"])
     got = rocs.cache_attention(cache, case["plan"], case["Q"], slots=case["slots"])
     assert torch.isnan(got).all()
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32])
+@pytest.mark.parametrize("dh,counts", [(128, [1, 1, 1]), (64, [2, 1, 3]), (128, [40, 300, 129]), (64, [200, 90, 30]), (32, [60, 2, 40])])
+@pytest.mark.parametrize("toward", ["first", "last"])
+def test_scores_that_grow_by_hundreds(dtype, dh, counts, toward):
+    """Keys that are multiples of one direction: scores climb (or fall) by about 25 per key, far beyond fp32's exponents over a
+    sequence; every row's softmax is all but its largest visible key's value."""
+    lens = [700, 400, 513]
+    case = build(dtype, counts, lens, 1, 2, dh, 16, seed=16)
+    direction = torch.zeros(dh, device="cuda")
+    direction[0] = 1.0
+    for r, L in enumerate(lens):
+        row = case["table"][case["slots"][r].long()]
+        for j in range(L):
+            at = j if toward == "last" else L - 1 - j
+            case["K"][int(row[j // 16]), j % 16] = (direction * 2.0 * at).to(dtype)
+    case["Q"][:] = (direction * 12.5).to(dtype)
+    cache = rocs.cache_create(case["K"], case["V"], case["table"], case["lens"])
+    got = rocs.cache_attention(cache, case["plan"], case["Q"], slots=case["slots"], scale=1.0)
+    O, A, S = plain.attention(case["K"], case["V"], case["table"], case["lens"], case["offsets"], case["Q"], case["slots"].tolist(), scale=1.0)
+    # the products are exact: one term each, 12.5 x an even number of at most 1400 (bf16 rounds it to 8 bits, alike for both)
+    assert torch.isfinite(got).all()
+    most = bound(dtype, O, A, torch.full_like(S, 64.0), 700, dh)
+    assert bool(((got.double() - O).abs() <= most).all())
+
+
+@pytest.mark.parametrize("dtype,dh,page", [(BF16, 64, 16), (BF16, 128, 24), (F32, 32, 8)])
+@pytest.mark.parametrize("R,n", [(130, 1), (200, 3), (200, 40), (300, 20), (140, 90)])
+def test_more_tiles_than_a_block_keeps(dtype, dh, page, R, n):
+    rng = random.Random(17)
+    lens = [rng.randint(0, 60) + n for _ in range(R)]
+    counts = [rng.randint(0, n) for _ in range(R)]
+    case = build(dtype, counts, lens, 1, 1, dh, page, seed=17)
+    begin = []
+    for c, L in zip(counts, lens):
+        begin += [max(0, (L - c + t) - 20) for t in range(c)]
+    check(case)
+    check(case, begin=torch.tensor(begin, dtype=torch.int32).cuda(), slopes=slopes(1))
+
+
+def test_refusals():
+    case = build(BF16, [1, 90], [400, 200], 2, 2, 64, 16, seed=18)
+    cache = rocs.cache_create(case["K"], case["V"], case["table"], case["lens"])
+    Q, plan, slots = case["Q"], case["plan"], case["slots"]
+    out = torch.full_like(Q, 7.0)
+
+    def refused(error, match=None, **how):
+        args = dict(slots=slots, out=out)
+        q = how.pop("Q", Q)
+        args.update(how)
+        with pytest.raises(error, match=match):
+            rocs.cache_attention(cache, plan, q, **args)
+
+    ints = lambda *v: torch.tensor(v, dtype=torch.int32, device="cuda")   # noqa: E731
+    refused(AssertionError, slots=ints(0))
+    refused(AssertionError, slots=slots.long())
+    refused(AssertionError, slots=slots.cpu())
+    refused(AssertionError, Q=Q[:5])
+    refused(AssertionError, Q=Q.float())
+    refused(AssertionError, Q=Q.cpu())
+    refused(AssertionError, Q=Q[:, :, :32])
+    refused(ValueError, Q=Q[0])
+    refused(rocs.RocsError, "invalid", Q=Q[:, :3].contiguous(), out=None)       # heads that do not share the key heads evenly
+    refused(AssertionError, slopes=slopes(3))
+    refused(AssertionError, begin=ints(0, 0))
+    refused(AssertionError, prefix=ints(0))
+    refused(rocs.RocsError, "invalid", prefix=ints(0, 0), causal=False)
+    refused(rocs.RocsError, "invalid", cap=-1.0)
+    refused(rocs.RocsError, "invalid", cap=float("inf"))
+    refused(rocs.RocsError, "invalid", scale=float("nan"))
+    refused(rocs.RocsError, "invalid", layer=1)
+    refused(rocs.RocsError, "invalid", layer=-1)
+    refused(rocs.RocsError, "workspace", workspace=torch.empty(64, dtype=torch.uint8, device="cuda"))
+    refused(AssertionError, workspace=torch.empty(1 << 20, dtype=torch.float32, device="cuda"))
+    wide = torch.empty((Q.shape[0], 4, 66), dtype=BF16, device="cuda")
+    refused(rocs.RocsError, "align", out=wide[:, :, :64])
+    refused(rocs.RocsError, "invalid", out=Q[:1].expand_as(Q))                  # rows that share memory
+    torch.cuda.synchronize()
+    assert torch.all(out == 7.0)
+    cache.close()
+    refused(ValueError, "closed")
+    with pytest.raises(rocs.RocsError):
+        rocs.cache_create(case["K"], case["V"], case["table"], torch.zeros(case["table"].shape[0] + 1, dtype=torch.int32, device="cuda")[1:])
+
+
+def test_views_of_the_pool_that_overlap_are_refused():
+    K = torch.zeros((4, 16, 2, 64), dtype=BF16, device="cuda")
+    table, lens = torch.zeros((2, 2), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
+    for view in (K[:1].expand(4, 16, 2, 64), K[:, :, :1].expand(4, 16, 2, 64)):
+        with pytest.raises(rocs.RocsError, match="invalid"):
+            rocs.cache_create(view, view, table, lens)
+    rocs.cache_create(K, K.clone(), table, lens)
