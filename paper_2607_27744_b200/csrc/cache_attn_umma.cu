@@ -155,11 +155,13 @@ __device__ __forceinline__ void transpose_pieces(uint4 (&v)[4], int lane) {
 }
 
 // 2^x for a pair on the FMA pipes: 2^n 2^f with n the nearest integer and a polynomial of degree 3 for 2^f on [-1/2, 1/2]
-// (fitted for the least relative error, 7.5e-5: a 26th of the rounding to bf16 that follows).  Below 2^-125 it stays there.
+// (fitted for the least relative error, 7.5e-5: a 26th of the rounding to bf16 that follows).  Below 2^-125 it stays there;
+// what is NaN, or too large for fp32, comes out as NaN, or so large that bf16 has an infinity for it.
 __device__ __forceinline__ uint64_t exp2_pair(uint64_t x2) {
   float x0, x1;
   unpack2(x2, x0, x1);
-  const uint64_t x = pack2(fmaxf(x0, -125.f), fmaxf(x1, -125.f));
+  // (fminf first: it takes NaN to 129, and 2^129 by the addition to the exponent is NaN)
+  const uint64_t x = pack2(fmaxf(fminf(x0, 129.f), -125.f), fmaxf(fminf(x1, 129.f), -125.f));
   constexpr float kMagic = 12582912.f;  // 1.5 x 2^23: the sum's last bits are the nearest integer
   const uint64_t t = fadd2(x, pack2(kMagic, kMagic));
   const uint64_t f = fadd2(x, ffma2(t, pack2(-1.f, -1.f), pack2(kMagic, kMagic)));

@@ -343,6 +343,27 @@ def test_scores_that_grow_by_hundreds(dtype, dh, counts, toward):
     assert bool(((got.double() - O).abs() <= most).all())
 
 
+@pytest.mark.parametrize("dtype,dh,n,page", [(BF16, 64, 130, 16), (BF16, 64, 300, 128), (BF16, 128, 130, 16), (BF16, 64, 50, 24), (BF16, 64, 1, 16),
+                                             (BF16, 128, 9, 64), (F32, 64, 20, 16)])
+@pytest.mark.parametrize("score", [60.0, 95.0, 1600.0, float("nan")])
+def test_one_key_far_above_all_others(dtype, dh, n, page, score):
+    """One key of each request, at another place of 16, whose score all rows see; far beyond fp32's exponents the softmax is its
+    value alone, and a row that sees a NaN is NaN."""
+    R, L = 16, 700
+    case = build(dtype, [n] * R, [L] * R, 1, 1, dh, page, seed=19)
+    case["K"][..., 0] = torch.where(case["K"][..., 0].isnan(), case["K"][..., 0], 0.0)
+    case["Q"][..., 0] = 8.0
+    for r in range(R):
+        j = 192 + r
+        row = case["table"][case["slots"][r].long()]
+        case["K"][int(row[j // page]), j % page, 0, 0] = score
+    if score == score:
+        check(case, scale=0.125)
+    else:
+        cache = rocs.cache_create(case["K"], case["V"], case["table"], case["lens"])
+        assert torch.isnan(rocs.cache_attention(cache, case["plan"], case["Q"], slots=case["slots"], scale=0.125)).all()
+
+
 @pytest.mark.parametrize("dtype,dh,page", [(BF16, 64, 16), (BF16, 128, 24), (F32, 32, 8)])
 @pytest.mark.parametrize("R,n", [(130, 1), (200, 3), (200, 40), (300, 20), (140, 90)])
 def test_more_tiles_than_a_block_keeps(dtype, dh, page, R, n):
