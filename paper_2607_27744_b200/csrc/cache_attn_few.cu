@@ -50,7 +50,8 @@ struct FewCfg {
   }
 };
 
-// What stands for "no reference yet": below every score, and finite, so that it needs no case of its own.
+// What stands for "no reference yet": finite, so that it needs no case of its own.  Scores below it weigh 0; a row that has no
+// others is computed again.
 constexpr float kNoReference = -3.0e38f;
 
 __device__ __forceinline__ void ldmatrix_x4(uint32_t addr, uint32_t (&r)[4]) {
@@ -410,7 +411,7 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
 #pragma unroll
         for (int c = 0; c < DH / 32; ++c) probe = fmaf(acc[i][c], 0.f, probe);
         const RowKeys rk = attn_row(p, e, t);
-        if (__any_sync(0xffffffffu, probe != 0.f))
+        if (__any_sync(0xffffffffu, probe != 0.f || ll == 0.f))
           attn_row_by_hand<DH>(p, e, kv_head_bytes, p.Q + (int64_t)(e.row0 + t) * p.q_row_bytes + h * p.q_head_bytes, rk, slope_of(p, h),
                                blk0 * kFewKeys, (blk0 + blocks) * kFewKeys, mm, ll, acc[i]);
         if (whole) {

@@ -318,6 +318,19 @@ def test_all_visible_scores_at_the_lowest_value_and_beyond():
     assert torch.isnan(got).all()
 
 
+@pytest.mark.parametrize("dh,page,counts", [(64, 16, [1, 1, 4]), (128, 64, [2, 16, 1]), (64, 24, [1, 4, 30]), (64, 16, [40, 300, 129])])
+def test_equal_scores_next_to_the_lowest_value(dh, page, counts):
+    """All visible scores are the same product, -3.08e38 in powers of two: the result is the mean of the values."""
+    case = build(BF16, counts, [90, 400, 300], 1, 1, dh, page, seed=20)
+    case["Q"].zero_()
+    case["Q"][..., 0] = 2.0 ** 63
+    case["K"][~torch.isnan(case["K"])] = -(2.0 ** 64)
+    got = rocs.cache_attention(rocs.cache_create(case["K"], case["V"], case["table"], case["lens"]), case["plan"], case["Q"],
+                               slots=case["slots"], scale=1.255)
+    O, A, S = plain.attention(case["K"], case["V"], case["table"], case["lens"], case["offsets"], case["Q"], case["slots"].tolist(), scale=1.255)
+    assert bool(((got.double() - O).abs() <= bound(BF16, O, A, torch.zeros_like(S), 400, dh)).all())
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32])
 @pytest.mark.parametrize("dh,counts", [(128, [1, 1, 1]), (64, [2, 1, 3]), (128, [40, 300, 129]), (64, [200, 90, 30]), (32, [60, 2, 40])])
 @pytest.mark.parametrize("toward", ["first", "last"])
