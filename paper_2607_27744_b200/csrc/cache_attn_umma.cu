@@ -728,6 +728,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       if (leads) {
         bad = there && (split ? ends[0].z + ends[kSide].z + ends[2 * kSide].z + ends[3 * kSide].z
                               : ends[side * 2 * kSide].z + ends[(side * 2 + 1) * kSide].z) != 0.f;
+        // Scores of 2^31 and more: their product with the scale is not rounded where the reference was, so that all weights may
+        // have come out as 0.
+        bad = bad || (sees && l_all == 0.f && keys.lo < (blk0 + n) * BK && keys.hi > blk0 * BK);
       }
       uint32_t redo = __ballot_sync(0xffffffffu, bad);
       while (redo != 0) {  // a row at a time, by the warp
