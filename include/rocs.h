@@ -378,6 +378,7 @@ rocs_status_t rocs_cache_compact(const rocs_cache_t* cache, int32_t* table_out, 
  *   O[i, h, :] = sum_j softmax_j(x) V_j over the visible j, zeros where none is.  H query heads, a multiple of the cache's
  *   H_kv: head h reads key head h / (H / H_kv).
  *   Q [N, H, dh], ld_qt, ld_qh and O [N, H, dh], ld_ot, ld_oh: strides of row and head (elements, of 16-byte multiples)
+ *   (0 in Q: one row, or one head, for all)
  * Keys that a row does not see have no influence on it, whatever they hold (NaN and Inf included).
  *   workspace >= rocs_cache_attention_workspace(cache, plan, H) bytes, 256-byte aligned; contents are overwritten
  */

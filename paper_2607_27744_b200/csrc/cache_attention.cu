@@ -364,7 +364,7 @@ rocs_status_t general_of(const CacheAttn& p, int32_t grid, cudaStream_t stream) 
 
 enum class Kind { kGeneral, kMma, kFew, kUmma };
 
-// Which kernel a call takes, and how its work is cut.
+// Which kernel a call takes, and how its work is cut.  q_spread: neither the rows nor the heads of Q are one broadcast.
 struct Choice {
   Kind kind;
   int32_t group, per_kv, heads;  // query heads per tile row, such groups per key head, groups in all
@@ -372,7 +372,7 @@ struct Choice {
   int64_t entries;
   bool by_request;  // no request has more than one tile
 };
-Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H, int path) {
+Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H, int path, bool q_spread) {
   Choice x{};
   const int32_t g = H / c->H_kv, sms = sms_of_device();
   int32_t most = 16;
@@ -397,7 +397,8 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H, int path) {
     // rows 28.3 / 28.7 / 29.8 and 28.7 / 32.3 / 47.9; 8 over 2000, 8 heads of 128: 40 / 64 / 100 rows 26.9 / 27.9 / 30.2 and 34.8 /
     // 37.6 / 58.8.  How many keys there are is known on the device only; the table's width says how many there may be.
     const bool many_keys = (int64_t)c->width * c->page >= 512;
-    if ((int64_t)plan->largest * g > (many_keys ? 32 : 128) && attn_umma_supported(c->dh, c->page)) {
+    // (its tensor map of Q takes no stride of 0)
+    if (q_spread && (int64_t)plan->largest * g > (many_keys ? 32 : 128) && attn_umma_supported(c->dh, c->page)) {
       x.kind = Kind::kUmma;
       x.block = kUmmaKeys;
       x.min_shift = 2;
@@ -452,8 +453,9 @@ extern "C" {
 
 size_t rocs_cache_attention_workspace(const rocs_cache_t* c, const rocs_plan_t* plan, int32_t H) {
   if (!c || !plan || H < 1 || H % c->H_kv != 0) return 0;
-  size_t most = 0;  // whichever path is in force when it is used
-  for (int path : {ROCS_PATH_AUTO, ROCS_PATH_GENERAL}) most = std::max(most, places(choose(c, plan, H, path), c->dh).bytes);
+  size_t most = 0;  // whichever path is in force when it is used, and whatever strides Q has
+  for (int path : {ROCS_PATH_AUTO, ROCS_PATH_GENERAL})
+    for (bool q_spread : {false, true}) most = std::max(most, places(choose(c, plan, H, path, q_spread), c->dh).bytes);
   return most;
 }
 
@@ -470,7 +472,7 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
   if ((H > 1 && ld_oh < c->dh) || (plan->N > 1 && ld_ot < c->dh)) return ROCS_ERR_INVALID_ARG;  // rows of O share no memory
   if (H > 65535) return ROCS_ERR_UNSUPPORTED;
   if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)c->dh);
-  const Choice x = choose(c, plan, H, kernel_path());
+  const Choice x = choose(c, plan, H, kernel_path(), (H == 1 || ld_qh > 0) && (plan->N == 1 || ld_qt > 0));
   const Places w = places(x, c->dh);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || bytes < w.bytes) return ROCS_ERR_WORKSPACE;
   if (x.entries > 0x7fffffffLL) return ROCS_ERR_UNSUPPORTED;
@@ -501,7 +503,6 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
   p.heads = x.heads;
   p.per_kv = x.per_kv;
   p.rows_per_tile = x.rows_per_tile;
-  p.R = plan->R;
   p.Q = static_cast<const uint8_t*>(Q);
   p.O = static_cast<uint8_t*>(O);
   p.q_row_bytes = ld_qt * es;

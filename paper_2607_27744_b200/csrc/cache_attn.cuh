@@ -47,7 +47,6 @@ struct CacheAttn {
   int32_t entries, causal;
   // query heads: `group` of them per tile row, `heads` groups, `per_kv` groups per key head
   int32_t group, heads, per_kv, rows_per_tile;  // rows_per_tile: of the batch
-  int32_t R;
   const uint8_t* Q;
   uint8_t* O;
   int64_t q_row_bytes, q_head_bytes, o_row_bytes, o_head_bytes;

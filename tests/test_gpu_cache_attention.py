@@ -153,6 +153,16 @@ def test_orders_of_the_pages_and_strided_rows(order, dtype, dh, counts):
     assert torch.all(room[0] == 9) and torch.all(room[N + 1] == 9) and torch.all(room[:, 0] == 9) and torch.all(room[:, :, dh:] == 9)
 
 
+@pytest.mark.parametrize("dtype,dh,counts", [(BF16, 64, [1, 1, 1]), (BF16, 128, [200, 3, 64]), (BF16, 64, [70, 33, 300]), (F32, 64, [20, 1, 5])])
+@pytest.mark.parametrize("over", ["rows", "heads", "both"])
+def test_queries_broadcast(dtype, dh, counts, over):
+    case = build(dtype, counts, [700, 100, 513], 2, 2, dh, 16, seed=21)
+    Q = case["Q"]
+    part = Q[:1 if over != "heads" else None, :1 if over != "rows" else None]
+    case["Q"] = part.expand_as(Q)
+    check(case)
+
+
 @pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
 @pytest.mark.parametrize("dtype,dh,counts", [(BF16, 64, [3, 1, 16]), (BF16, 128, [130, 40, 300]), (BF16, 64, [70, 300, 20]), (F32, 64, [30, 1, 9]),
                                              (BF16, 32, [40, 9, 30])])
