@@ -439,6 +439,13 @@ bool strides_ok(int64_t ld_row, int64_t ld_head, int64_t es) {
   return ld_row >= 0 && ld_head >= 0 && ld_row * es % 16 == 0 && ld_head * es % 16 == 0;
 }
 
+// Whether rows of O share memory: the larger of the two strides has to span all that the smaller one does.
+bool shares_memory(int64_t rows, int64_t ld_row, int64_t heads, int64_t ld_head, int64_t dh) {
+  if (rows > 1 && heads > 1)
+    return ld_row < ld_head ? ld_row < dh || (ld_head - dh) / ld_row < rows - 1 : ld_head < dh || (ld_row - dh) / ld_head < heads - 1;
+  return (heads > 1 && ld_head < dh) || (rows > 1 && ld_row < dh);
+}
+
 }  // namespace
 
 rocs_status_t attn_general(rocs_dtype_t dt, const CacheAttn& p, int32_t grid, cudaStream_t stream) {
@@ -469,9 +476,10 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
   if (!Q || !O) return ROCS_ERR_INVALID_ARG;
   const int64_t es = (int64_t)elem_size(c->dtype);
   if (!aligned16(Q) || !aligned16(O) || !strides_ok(ld_qt, ld_qh, es) || !strides_ok(ld_ot, ld_oh, es)) return ROCS_ERR_ALIGNMENT;
-  if ((H > 1 && ld_oh < c->dh) || (plan->N > 1 && ld_ot < c->dh)) return ROCS_ERR_INVALID_ARG;  // rows of O share no memory
+  if (shares_memory(plan->N, ld_ot, H, ld_oh, c->dh)) return ROCS_ERR_INVALID_ARG;
   if (H > 65535) return ROCS_ERR_UNSUPPORTED;
   if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)c->dh);
+  if (!std::isfinite(scale * kLog2e) || (cap > 0.f && !std::isfinite(scale / cap))) return ROCS_ERR_INVALID_ARG;
   const Choice x = choose(c, plan, H, kernel_path(), (H == 1 || ld_qh > 0) && (plan->N == 1 || ld_qt > 0));
   const Places w = places(x, c->dh);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || bytes < w.bytes) return ROCS_ERR_WORKSPACE;

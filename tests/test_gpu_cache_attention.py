@@ -446,6 +446,22 @@ def test_refusals():
         rocs.cache_create(case["K"], case["V"], case["table"], torch.zeros(case["table"].shape[0] + 1, dtype=torch.int32, device="cuda")[1:])
 
 
+def test_outputs_that_share_memory_and_scales_without_a_value_are_refused():
+    case = build(BF16, [1, 90], [400, 200], 2, 2, 64, 16, seed=18)
+    cache = rocs.cache_create(case["K"], case["V"], case["table"], case["lens"])
+    flat = torch.full((91 * 4 * 64 + 64,), 7.0, dtype=BF16, device="cuda")
+    for strides in ((64, 64, 1), (128, 64, 1), (248, 64, 1), (64, 90 * 64, 1), (0, 64, 1), (256, 0, 1)):
+        with pytest.raises(rocs.RocsError, match="invalid"):
+            rocs.cache_attention(cache, case["plan"], case["Q"], slots=case["slots"], out=flat.as_strided((91, 4, 64), strides))
+    for how in (dict(scale=3e38), dict(scale=1.0, cap=1e-39)):
+        with pytest.raises(rocs.RocsError, match="invalid"):
+            rocs.cache_attention(cache, case["plan"], case["Q"], slots=case["slots"], out=flat[:91 * 256].view(91, 4, 64), **how)
+    torch.cuda.synchronize()
+    assert torch.all(flat == 7.0)
+    check(case, out=flat.as_strided((91, 4, 64), (64, 91 * 64, 1)))
+    check(case, out=flat.as_strided((91, 4, 64), (256, 64, 1)))
+
+
 def test_views_of_the_pool_that_overlap_are_refused():
     K = torch.zeros((4, 16, 2, 64), dtype=BF16, device="cuda")
     table, lens = torch.zeros((2, 2), dtype=torch.int32, device="cuda"), torch.zeros(2, dtype=torch.int32, device="cuda")
