@@ -310,7 +310,7 @@ rocs_status_t rocs_linear_normed(rocs_dtype_t dtype, rocs_norm_t kind, int64_t M
  * A cache names these arrays (16-byte aligned, device memory of the caller, who may read and write them in stream
  * order) and owns no device memory; creating and destroying it enqueues nothing.  Lengths outside 0..width * page count
  * as the nearer end.  An entry of the table outside 0..n_pages-1 reads as a page of zeros and is never written through.
- * Limits: width <= 2^20, width * page and page * H_kv * dh < 2^31, dh <= 256, dh * sizeof(element) a multiple of 16.
+ * Limits: width <= 2^20, width * page <= 2^30, page * H_kv * dh < 2^31, dh <= 256, dh * sizeof(element) a multiple of 16.
  *
  * The calls that keep the books (extend, fork, truncate, compact) run on the device without the host: no
  * synchronisation, and a captured one works on what it finds at each replay.  They are all or nothing: a call that

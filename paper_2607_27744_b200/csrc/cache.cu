@@ -601,8 +601,8 @@ rocs_status_t rocs_cache_create(rocs_cache_t** out, rocs_dtype_t dtype, int32_t 
       if (*d.ld < span) return ROCS_ERR_INVALID_ARG;
       span += (d.n - 1) * *d.ld;
     }
-  // (width: prefix sums over 1024 rows of the table stay in 32 bits)
-  if (dh > 256 || (int64_t)width * page > 0x7fffffffLL || width > (1 << 20) || (int64_t)page * H_kv * dh > 0x7fffffffLL)
+  // (width: prefix sums over 1024 rows of the table stay in 32 bits; positions: so does the next multiple of a block or a page)
+  if (dh > 256 || (int64_t)width * page > (1ll << 30) || width > (1 << 20) || (int64_t)page * H_kv * dh > 0x7fffffffLL)
     return ROCS_ERR_UNSUPPORTED;
   rocs_cache* c = new (std::nothrow) rocs_cache{dtype, layers, n_pages, page, H_kv, dh, K, V, ld_layer, ld_page, ld_token, ld_head,
                                                 n_slots, width, table, lens, refs};

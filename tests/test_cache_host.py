@@ -61,6 +61,15 @@ def test_what_a_cache_may_be(lib, change, code):
     lib.rocs_cache_destroy(handle)
 
 
+@pytest.mark.parametrize("page,width,code", [(1 << 10, 1 << 20, 0), ((1 << 10) + 1, 1 << 20, UNSUPPORTED), (65537, 16383, 0), (65537, 16384, UNSUPPORTED),
+                                             (65537, 32767, UNSUPPORTED)])
+def test_how_long_a_slot_may_be(lib, page, width, code):
+    """Positions stay far enough below 2^31 that the end of their last page or block does too."""
+    got, handle = create(lib, page=page, width=width, H=1, ld_head=0, ld_token=64, ld_page=64 * page, ld_layer=640 * page)
+    assert got == code
+    lib.rocs_cache_destroy(handle)
+
+
 def test_calls_on_a_cache(lib):
     _, c = create(lib)
     _, bare = create(lib, refs=None)
