@@ -174,6 +174,20 @@ __host__ __device__ constexpr int gen_row_bytes(int dh) { return dh * (int)sizeo
 template <typename T>
 constexpr int gen_smem(int dh) { return kGenRows * dh * 4 + 4 * kGenKeys * gen_row_bytes<T>(dh); }
 
+template <typename T>
+__device__ __forceinline__ void unpack_vec(const uint4& raw, float (&v)[16 / sizeof(T)]) {
+  const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    if constexpr (sizeof(T) == 4) {
+      v[x] = __uint_as_float(w[x]);
+    } else {
+      v[2 * x] = __uint_as_float(w[x] << 16);
+      v[2 * x + 1] = __uint_as_float(w[x] & 0xffff0000u);
+    }
+  }
+}
+
 template <typename T, int NV>
 __global__ void __launch_bounds__(kGenThreads) general_kernel(const CacheAttn p) {
   extern __shared__ __align__(16) uint8_t smem[];
@@ -197,15 +211,26 @@ __global__ void __launch_bounds__(kGenThreads) general_kernel(const CacheAttn p)
     const int64_t kv_head_bytes = kv_head * p.head_bytes;
     const int32_t rows = e.count * p.group;
     __syncthreads();  // the piece in front is done with shared memory
-    for (int32_t x = threadIdx.x; x < kGenRows * dh; x += kGenThreads) {
-      const int32_t row = x / dh, c = x - row * dh;
-      float v = 0.f;
-      if (row < rows) {
-        const uint8_t* q = p.Q + (int64_t)(e.row0 + row / p.group) * p.q_row_bytes + (walk.head * p.group + row % p.group) * p.q_head_bytes;
-        if constexpr (sizeof(T) == 4) v = reinterpret_cast<const float*>(q)[c];
-        else v = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(q)[c]);
-      }
-      qs[x] = v * p.scale;
+    // (all of a thread's vectors are asked for before the first is stored: a trip to memory each would be most of a short piece)
+    constexpr int kPer = 16 / (int)sizeof(T), kQVecs = (NV * (int)sizeof(T) + 3) / 4;
+    uint4 raw_q[kQVecs];
+#pragma unroll
+    for (int i = 0; i < kQVecs; ++i) {
+      const int32_t x = threadIdx.x + i * kGenThreads, row = x / vecs;
+      raw_q[i] = make_uint4(0u, 0u, 0u, 0u);
+      if (row < min(rows, kGenRows))
+        raw_q[i] = *reinterpret_cast<const uint4*>(p.Q + (int64_t)(e.row0 + row / p.group) * p.q_row_bytes +
+                                                   (walk.head * p.group + row % p.group) * p.q_head_bytes + (x - row * vecs) * 16);
+    }
+#pragma unroll
+    for (int i = 0; i < kQVecs; ++i) {
+      const int32_t x = threadIdx.x + i * kGenThreads;
+      if (x >= kGenRows * vecs) continue;
+      float q[kPer];
+      unpack_vec<T>(raw_q[i], q);
+#pragma unroll
+      for (int c = 0; c < kPer; c += 4)
+        *reinterpret_cast<float4*>(qs + x * kPer + c) = make_float4(q[c] * p.scale, q[c + 1] * p.scale, q[c + 2] * p.scale, q[c + 3] * p.scale);
     }
     RowKeys keys[4];
     float slope[4], m[4], l[4], acc[4][NV];
@@ -228,16 +253,24 @@ __global__ void __launch_bounds__(kGenThreads) general_kernel(const CacheAttn p)
     }
     const int32_t blk0 = e.blk0 + walk.block0(p), blocks = e.blocks > 0 ? walk.blocks(p) : 0;
     const int32_t last_key = min(e.L, p.causal ? max(e.pos0 + e.count, e.prefix) : e.L);  // one past the last that any row sees
+    // A lane looks up a key of the next block to load, a block ahead: a trip to memory in front of another.
+    auto look_up = [&](int32_t b) {
+      const int32_t j = (blk0 + b) * kGenKeys + lane;
+      return b < blocks && j < last_key ? key_offset(p, e.slot, j) : -1;
+    };
+    int64_t ahead = look_up(0);
     auto load = [&](int32_t b) {
       const uint32_t dst = kv_addr + (b & 1) * 2 * block_bytes;
-      for (int32_t x = threadIdx.x; x < kGenKeys * vecs; x += kGenThreads) {
-        const int32_t row = x / vecs, v = x - row * vecs, j = (blk0 + b) * kGenKeys + row;
-        const int64_t at = j < last_key ? key_offset(p, e.slot, j) : -1;
+#pragma unroll 4
+      for (int32_t x = threadIdx.x; x < kGenKeys * vecs; x += kGenThreads) {  // (a multiple of 32 of them: whole warps)
+        const int32_t row = x / vecs, v = x - row * vecs;
+        const int64_t at = __shfl_sync(0xffffffffu, ahead, row);
         const int64_t off = at >= 0 ? at + kv_head_bytes + v * 16 : 0;
         cp_async16(dst + row * row_bytes + v * 16, p.K + off, at >= 0);
         cp_async16(dst + block_bytes + row * row_bytes + v * 16, p.V + off, at >= 0);
       }
       cp_async_commit();
+      ahead = look_up(b + 1);
     };
     if (blocks > 0) load(0);
     for (int32_t b = 0; b < blocks; ++b) {
@@ -255,20 +288,11 @@ __global__ void __launch_bounds__(kGenThreads) general_kernel(const CacheAttn p)
       float s[4] = {0.f, 0.f, 0.f, 0.f};
       const float* q = qs + warp * 4 * dh;
       const uint8_t* kr = kb + lane * row_bytes;
+#pragma unroll 4
       for (int32_t v = 0; v < vecs; ++v) {
         const uint4 raw = *reinterpret_cast<const uint4*>(kr + v * 16);
-        constexpr int kPer = 16 / (int)sizeof(T);
         float k[kPer];
-        if constexpr (sizeof(T) == 4) {
-          k[0] = __uint_as_float(raw.x); k[1] = __uint_as_float(raw.y); k[2] = __uint_as_float(raw.z); k[3] = __uint_as_float(raw.w);
-        } else {
-          const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-          for (int x = 0; x < 4; ++x) {
-            k[2 * x] = __uint_as_float(w[x] << 16);
-            k[2 * x + 1] = __uint_as_float(w[x] & 0xffff0000u);
-          }
-        }
+        unpack_vec<T>(raw, k);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
 #pragma unroll
