@@ -163,10 +163,12 @@ rocs_status_t join_parts(const CacheAttn& p, int32_t rows, int32_t grid, cudaStr
 
 // ---- general kernel -------------------------------------------------------------------------------
 // 16 rows x blocks of 32 keys on fp32 FMAs, storage fp32 or bf16.  Queries are scaled before the product and scores stay in
-// natural units up to their difference from the reference: whatever scaled score fp32 can hold is a score.  A warp has 4 rows: its lanes are the block's keys for
-// the scores (one key's row of shared memory each, 4 queries broadcast) and output columns for P V (the probabilities
-// broadcast).  K and V blocks are fetched with cp.async, the next while one is used.  Bound by shared-memory reads (5 per
-// 16 FMAs of a score); the rows of a chunk and the keys of a long history are shared over CTAs by the line of work.
+// natural units up to their difference from the reference: whatever scaled score fp32 can hold is a score.  A warp has 4 rows:
+// its lanes are the block's keys for the scores (one key's row of shared memory each, 4 queries broadcast) and output columns
+// for P V (the probabilities broadcast).  K and V blocks are fetched with cp.async, the next while one is used.
+// Long calls are bound by shared-memory reads (5 per 16 FMAs of a score, 3 per 8 of a value; 8 chunks of 200 events over 1500
+// keys, 8 heads of 64: 250 us, 20 TFLOP/s), short ones by their chain: of 19 us (2 chunks over 60 keys) 9 are the launches and
+// the line of work, 3.5 a piece's beginning and end, 3 a block.  Two output columns in one read were slower (305 us).
 constexpr int kGenThreads = 128, kGenRows = 16, kGenKeys = 32;
 
 template <typename T>
@@ -204,6 +206,9 @@ __global__ void __launch_bounds__(kGenThreads) general_kernel(const CacheAttn p)
   uint8_t* kv = smem + kGenRows * dh * 4;  // [2 stages][K, V][32 keys]
   const uint32_t kv_addr = ptx::smem_u32(kv);
   const int32_t block_bytes = kGenKeys * row_bytes;
+  // the vectors of a block that a thread loads: kGenThreads after one another
+  const int32_t load_row = threadIdx.x / vecs, load_vec = threadIdx.x - load_row * vecs;
+  const int32_t row_step = kGenThreads / vecs, vec_step = kGenThreads - row_step * vecs;
 
   for (; walk.more(); walk.next(p, view)) {
     const AttnEntry e = view.entry[walk.entry];
@@ -262,12 +267,17 @@ __global__ void __launch_bounds__(kGenThreads) general_kernel(const CacheAttn p)
     auto load = [&](int32_t b) {
       const uint32_t dst = kv_addr + (b & 1) * 2 * block_bytes;
 #pragma unroll 4
-      for (int32_t x = threadIdx.x; x < kGenKeys * vecs; x += kGenThreads) {  // (a multiple of 32 of them: whole warps)
-        const int32_t row = x / vecs, v = x - row * vecs;
+      for (int32_t row = load_row, v = load_vec; row < kGenKeys;) {  // (a multiple of 32 of them: whole warps)
         const int64_t at = __shfl_sync(0xffffffffu, ahead, row);
         const int64_t off = at >= 0 ? at + kv_head_bytes + v * 16 : 0;
         cp_async16(dst + row * row_bytes + v * 16, p.K + off, at >= 0);
         cp_async16(dst + block_bytes + row * row_bytes + v * 16, p.V + off, at >= 0);
+        row += row_step;
+        v += vec_step;
+        if (v >= vecs) {
+          v -= vecs;
+          ++row;
+        }
       }
       cp_async_commit();
       ahead = look_up(b + 1);
@@ -305,23 +315,36 @@ __global__ void __launch_bounds__(kGenThreads) general_kernel(const CacheAttn p)
           }
       }
       float pr[4];
+      bool moves = false;
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         float x = s[i];
         if (p.cap > 0.f) x = p.cap * tanhf(x);
         if (p.slopes) x -= slope[i] * fabsf((float)(keys[i].pos - j));
         if (!full && (j < keys[i].lo || j >= keys[i].hi)) x = -INFINITY;
-        float mx = x;
+        s[i] = x;
+        moves |= x > m[i] + 8.f;  // (from -inf: any score)
+      }
+      // a row's reference moves where a score passes it by e^8, which fp32 sums have room for
+      if (__any_sync(0xffffffffu, moves)) {
 #pragma unroll
-        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-        const float m_new = fmaxf(m[i], mx);
-        const float a = m[i] == m_new ? 1.f : exp2f((m[i] - m_new) * kLog2e);  // (both -inf: nothing yet)
-        pr[i] = x == -INFINITY ? 0.f : exp2f((x - m_new) * kLog2e);
-        l[i] = fmaf(l[i], a, pr[i]);
-        m[i] = m_new;
-        if (a != 1.f)
+        for (int i = 0; i < 4; ++i) {
+          float mx = s[i];
 #pragma unroll
-          for (int c = 0; c < NV; ++c) acc[i][c] *= a;
+          for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+          if (mx > m[i] + 8.f) {  // a row's own decision
+            const float a = exp2f((m[i] - mx) * kLog2e);
+            m[i] = mx;
+            l[i] *= a;
+#pragma unroll
+            for (int c = 0; c < NV; ++c) acc[i][c] *= a;
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        pr[i] = s[i] == -INFINITY ? 0.f : exp2f((s[i] - m[i]) * kLog2e);
+        l[i] += pr[i];
       }
       *reinterpret_cast<float4*>(probs[warp][lane]) = make_float4(pr[0], pr[1], pr[2], pr[3]);
       __syncwarp();
