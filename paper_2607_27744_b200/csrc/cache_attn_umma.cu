@@ -10,14 +10,16 @@
 // Tensor memory: S of both sides (128 columns each), O of both sides.  P (bf16 pairs) takes the place of the S that it comes
 // from, each half of a row in its own half of the columns; the products of a side are issued in the order P_j V_j, S_{j+1},
 // and run in that order, so nobody waits for the columns to come free, and the arrival of S_{j+1} says that O holds
-// everything up to P_j V_j.  While a side's products run, the other side's softmax does: the products of a block pair take
-// 2048 cycles (heads of 128) and its exponentials the same, so what bounds the kernel is how well the two overlap.
+// everything up to P_j V_j.  P_j is announced in two parts: the products of the first begin while the second is made.  While
+// a side's products run, the other side's softmax does: the products of a block pair take 2048 cycles (heads of 128) and its
+// exponentials the same, so what bounds the kernel is how well the two overlap.
 //
 // Blocks go from the last key to the first: masks (the chunk's own keys) come first, and a score that falls with distance
 // is largest there.  A row's reference is the maximum of the first block in which it sees a key; other blocks need no
 // maximum.  It moves up where a block's sum passes 2^40, by that sum's exponent, before the next block: both threads of the
 // row read what the other's half summed to, and scale O and their sums by the same power of two.  A probability keeps its
-// 8 bits wherever the reference is, sums are fp32.  All decisions are a row's own: its bits do not depend on other rows.
+// 8 bits wherever the reference is, sums are fp32.  All decisions are a row's own: its bits do not depend on other rows'
+// values.
 //
 // A row whose scores pass its reference by more than fp32's range within one block, or whose masked keys hold NaN or Inf
 // values (weight 0, but 0 x Inf is not 0), comes out non-finite and is computed again from the keys that it sees, by a warp.
@@ -52,8 +54,8 @@ struct UmmaCfg {
   static constexpr uint32_t kOffMax = kOffSum + 16 * kSide * 4;       // [2 sides][2 halves][128] maxima of a block
   static constexpr uint32_t kOffEnd = kOffMax + 4 * kSide * 4;        // [2 sides][2 halves][128] (reference, sum, probe, -)
   static constexpr uint32_t kOffBar = kOffEnd + 4 * kSide * 16;
-  static constexpr uint32_t kQFull = kOffBar, kQEmpty = kQFull + 8, kSFull = kQEmpty + 8, kPFull = kSFull + 16, kOFull = kPFull + 16,
-                            kTail = kOFull + 16, kDrain = kTail + 8, kPair = kDrain + 8, kQuad = kPair + 64, kKFull = kQuad + 32,
+  static constexpr uint32_t kQFull = kOffBar, kQEmpty = kQFull + 8, kSFull = kQEmpty + 8, kPFull = kSFull + 16,
+                            kPHalf = kPFull + 16, kOFull = kPHalf + 16, kTail = kOFull + 16, kDrain = kTail + 8, kPair = kDrain + 8, kQuad = kPair + 64, kKFull = kQuad + 32,
                             kKEmpty = kKFull + 8 * kStages,
                             kVFull = kKEmpty + 8 * kStages, kVEmpty = kVFull + 8 * kStages, kOffTmem = kVEmpty + 8 * kStages,
                             kOffAbort = kOffTmem + 8;
@@ -181,6 +183,10 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
             const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CacheAttn p) {
   using C = UmmaCfg<DH>;
   constexpr int kStages = C::kStages;
+  // How many of a half's four groups of 16 keys are announced when their P is there, in front of the others (0: all at once): their
+  // products run while the others' exponentials do.  Long chunk: none 500 us, one 499, two 481, three 482; candidates 127.0 and
+  // 126.2 with two; capped scores wait longer for a second arrival than they gain (first visits 131.8 and 133.9).
+  constexpr int kFirst = CAP ? 0 : 2;
   extern __shared__ __align__(1024) uint8_t smem[];
   __shared__ AttnLine line_mem;
   const uint32_t sb = smem_u32(smem);
@@ -198,6 +204,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
     init(C::kQEmpty, 1, 1);
     init(C::kSFull, 2, 1);
     init(C::kPFull, 2, 8);
+    init(C::kPHalf, 2, 8);
     init(C::kOFull, 2, 1);
     init(C::kTail, 1, 1);
     init(C::kDrain, 1, 1);
@@ -340,17 +347,31 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
                   dk + st * (C::kTileBytes >> 4) + (k / 4) * (C::kBoxBytes >> 4) + 2 * (k % 4), idesc_s, k != 0 ? 1u : 0u);
         umma_commit(sb + C::kSFull + 8 * side);
       };
-      auto issue_pv = [&](int side, uint32_t st, bool first) {  // 16 keys of P: 8 columns, in their half of the row's S
+      // 16 keys of P: 8 columns, in their half of the row's S; keys [from, to) x 16 of either half
+      auto issue_pv = [&](int side, uint32_t st, bool first, auto from, auto to) {
 #pragma unroll
         for (int k = 0; k < BK / 16; ++k)
-          umma_ts(tmem + C::kColO + side * DH, tmem + side * 128 + (k / 4) * 64 + (k % 4) * 8,
-                  dv + st * (C::kTileBytes >> 4) + k * (16 * 128 / 16), idesc_o, first && k == 0 ? 0u : 1u);
+          if (k % 4 >= decltype(from)::value && k % 4 < decltype(to)::value)
+            umma_ts(tmem + C::kColO + side * DH, tmem + side * 128 + (k / 4) * 64 + (k % 4) * 8,
+                    dv + st * (C::kTileBytes >> 4) + k * (16 * 128 / 16), idesc_o, first && k == 0 ? 0u : 1u);
       };
       auto wait_k = [&]() { return wait(sb + C::kKFull + 8 * (kt % kStages), (kt / kStages) & 1, 6); };
       auto wait_v = [&]() { return wait(sb + C::kVFull + 8 * (vt % kStages), (vt / kStages) & 1, 8); };
-      auto wait_p = [&](int side) {
-        if (!wait(sb + C::kPFull + 8 * side, cnt_p[side] & 1, 7)) return false;
-        ++cnt_p[side];
+      auto wait_p = [&](int side, bool half) {
+        if (!wait(sb + (half ? C::kPHalf : C::kPFull) + 8 * side, cnt_p[side] & 1, 7)) return false;
+        if (!half) ++cnt_p[side];
+        return true;
+      };
+      auto add_pv = [&](int side, uint32_t st, bool first) {  // false: P did not come
+        using std::integral_constant;
+        if (kFirst > 0) {
+          if (!wait_p(side, true)) return false;
+          tc_fence_after_sync();
+          issue_pv(side, st, first, integral_constant<int, 0>(), integral_constant<int, kFirst>());
+        }
+        if (!wait_p(side, false)) return false;
+        tc_fence_after_sync();
+        issue_pv(side, st, first, integral_constant<int, kFirst>(), integral_constant<int, 4>());
         return true;
       };
       auto k_done = [&]() { umma_commit(sb + C::kKEmpty + 8 * (kt++ % kStages)); };
@@ -371,9 +392,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
           for (int32_t i = 0; i < n && ok; ++i) {
             for (int s = 0; s < 2; ++s) {
               if (s == 0 && (!wait_v() || (i + 1 < n && !wait_k()))) break;  // long there, as a rule: not behind the wait for P
-              if (!wait_p(s)) break;
-              tc_fence_after_sync();
-              issue_pv(s, vt % kStages, i == 0);
+              if (!add_pv(s, vt % kStages, i == 0)) break;
               if (i + 1 < n) issue_s(s, s, kt % kStages);
               else umma_commit(sb + C::kOFull + 8 * s);
             }
@@ -395,9 +414,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
           if (n <= 2) umma_commit(sb + C::kQEmpty);
           for (int32_t i = 0; i < n; ++i) {
             const int s = i & 1;
-            if (!wait_v() || (i + 2 < n && !wait_k()) || !wait_p(s)) break;
-            tc_fence_after_sync();
-            issue_pv(s, vt % kStages, i < 2);
+            if (!wait_v() || (i + 2 < n && !wait_k()) || !add_pv(s, vt % kStages, i < 2)) break;
             v_done();
             if (i + 2 < n) {
               issue_s(s, 0, kt % kStages);
@@ -480,7 +497,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
         if (!mbar_wait_suspended(sb + C::kSFull + 8 * side, cnt_s & 1, abort_flag, p.status, kStatusCache | 10)) { aborted = true; break; }
         tc_fence_after_sync();
         const int32_t b0 = (blk0 + n - 1 - i) * BK, j0 = b0 + half * 64;  // the block's first key, this thread's
-        const bool all_begun = b0 >= lo_most, none_ended = b0 + BK <= hi_least;  // what masks may be left out
+        // what masks may be left out, by the keys of this half (long chunk: 492 us, by those of the whole block 504 us), or of the
+        // block where scores are capped (first visits: 133.5 and 132.3 us)
+        const bool all_begun = (CAP ? b0 : j0) >= lo_most, none_ended = (CAP ? b0 + BK : j0 + 64) <= hi_least;
         auto mask = [&](int c0, uint32_t (&s)[16]) {
           if (!all_begun) {
             const int32_t lo = keys.lo - j0 - c0;
@@ -600,6 +619,12 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
               pk[x / 2] = bf16_pair(p0, p1);
             }
             tmem_st_x8(t_s + c * 8, pk);
+            if (c + 1 == kFirst) {  // the products of these keys may begin
+              tmem_st_wait();
+              tc_fence_before_sync();
+              __syncwarp();
+              if (lane == 0) mbar_arrive(sb + C::kPHalf + 8 * side);
+            }
           }
         };
         // blocks without a mask on code of their own (long chunk: 531 us on one for both) where scores are not capped (first
