@@ -659,6 +659,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       tc_fence_after_sync();
       const int32_t width = split ? DH / 4 : DH / 2, col0 = (split ? side * 2 + half : half) * width;
       const uint32_t t_a = t_lane + C::kColO + (split ? 0 : side * DH) + col0, t_b = t_lane + C::kColO + DH + col0;
+      // A side without a block of this piece has met nobody since the end of the piece in front, where its first half may still
+      // be reading the probes of both.  (Otherwise the arrival of O, for which all warps of the side have brought P, comes behind.)
+      if (first >= n && !meet(false)) break;
       ends[(side * 2 + half) * kSide] = make_float4(m, l, 0.f, 0.f);
       if (!meet(split)) break;
       float wa = 1.f, wb = 0.f, m_all = m, l_all;
