@@ -300,12 +300,28 @@ __device__ __forceinline__ float ex2_approx(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
-// tanh(t) = 1 - 2 / (1 + e^2t), absolute error about 1e-7 (two instructions of the special-function unit; tanh.approx is
-// one, and 2^-11 off, which capped scores of 50 would show).
-__device__ __forceinline__ float tanh_fast(float t) {
+// tanh(t) as 1 - 2 / (1 + e^2t), absolute error about 1e-7 (two instructions of the special-function unit; tanh.approx is one,
+// and 2^-11 off, which capped scores of 50 would show).  A score has that cap times: for caps of up to kShortCap, where it is
+// 6e-6, or scores beyond 3/4 of the cap.
+constexpr float kShortCap = 64.f;
+__device__ __forceinline__ float tanh_far(float t) {
   float r;
   asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + ex2_approx(t * 2.8853900817779268f)));
   return fmaf(-2.f, r, 1.f);
+}
+// tanh(t) to 1.7e-7 of its value, however small: a cap far above the scores (a caller's "none") leaves nothing of an absolute
+// error.  Up to 3/4 t P(t^2), fitted for the least relative error (3e-8, 1.3e-7 with fp32's roundings).
+constexpr float kTanhRange = 0.75f;
+constexpr float kTanh1 = -0.3333306908607483f, kTanh2 = 0.1332651972770691f, kTanh3 = -0.053390201181173325f,
+                kTanh4 = 0.01966479979455471f, kTanh5 = -0.004769410938024521f;
+__device__ __forceinline__ float tanh_of(float t) {
+  const float u = t * t;
+  float r = fmaf(kTanh5, u, kTanh4);
+  r = fmaf(r, u, kTanh3);
+  r = fmaf(r, u, kTanh2);
+  r = fmaf(r, u, kTanh1);
+  const float near = fmaf(r, u, 1.f) * t, far = tanh_far(t);  // (both: a branch around either costs more)
+  return fabsf(t) <= kTanhRange ? near : far;
 }
 
 __device__ __forceinline__ void cp_async16(uint32_t dst, const void* src, bool there) {
@@ -359,7 +375,7 @@ __device__ __forceinline__ void attn_row_by_hand(const CacheAttn& p, const AttnE
         }
       }
       x = s * p.scale;
-      if (p.cap > 0.f) x = p.cap * tanh_fast(x);
+      if (p.cap > 0.f) x = p.cap * tanh_of(x);
       if (p.slopes) x -= slope * fabsf((float)(keys.pos - j));
     }
     float mx = x;

@@ -285,7 +285,7 @@ few_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CU
             const float away = (float)(pos[n][i] - j0 - lane / 4);
 #pragma unroll
             for (int c = i; c < 4; c += 2) {
-              if (p.cap > 0.f) x[n][c] = p.cap * tanh_fast(x[n][c]);
+              if (p.cap > 0.f) x[n][c] = p.cap * tanh_of(x[n][c]);
               x[n][c] = fmaf(-slope[n][i], fabsf(away - (c / 2) * 8), x[n][c]);
             }
           }

@@ -122,17 +122,27 @@ __device__ __forceinline__ uint64_t fmul2(uint64_t a, uint64_t b) {
   asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(d) : "l"(a), "l"(b));
   return d;
 }
-// tanh of a pair within [-3/4, 3/4]: t P(t^2), fitted for the least absolute error, 3.6e-6 (two instructions of the
-// special-function unit per value and a third for its weight would be three times what the kernel waits for without a cap).
-// `u` receives t^2.
+// tanh of a pair within [-3/4, 3/4] as t P(t^2) (two instructions of the special-function unit per value and a third for its
+// weight would be three times what the kernel waits for without a cap).  `u` receives t^2.  SHORT: fitted for the least absolute
+// error, 3.6e-6, which a score has cap times: for caps of up to kShortCap, where that is 2.3e-4, an eighth of what rounding its
+// weight to bf16 changes it by.  Otherwise tanh_of's, right to 1.3e-7 of its value whatever the cap (first visits, cap 30: 133 us
+// with the short one, 142 us with the long one; candidates, cap 30: 162 and 178 us).
+template <bool SHORT>
 __device__ __forceinline__ uint64_t tanh_pair(uint64_t t, uint64_t& u) {
   u = fmul2(t, t);
-  uint64_t r = ffma2(u, pack2(-0.03377828374505043f, -0.03377828374505043f), pack2(0.1257709264755249f, 0.1257709264755249f));
-  r = ffma2(r, u, pack2(-0.3322276473045349f, -0.3322276473045349f));
-  r = ffma2(r, u, pack2(0.9999555945396423f, 0.9999555945396423f));
-  return fmul2(r, t);
+  if constexpr (SHORT) {
+    uint64_t r = ffma2(u, pack2(-0.03377828374505043f, -0.03377828374505043f), pack2(0.1257709264755249f, 0.1257709264755249f));
+    r = ffma2(r, u, pack2(-0.3322276473045349f, -0.3322276473045349f));
+    r = ffma2(r, u, pack2(0.9999555945396423f, 0.9999555945396423f));
+    return fmul2(r, t);
+  }
+  uint64_t r = ffma2(u, pack2(kTanh5, kTanh5), pack2(kTanh4, kTanh4));
+  r = ffma2(r, u, pack2(kTanh3, kTanh3));
+  r = ffma2(r, u, pack2(kTanh2, kTanh2));
+  r = ffma2(r, u, pack2(kTanh1, kTanh1));
+  return fmul2(ffma2(r, u, pack2(1.f, 1.f)), t);
 }
-constexpr float kTanhRange2 = 0.5625f;  // square of the range
+constexpr float kTanhRange2 = kTanhRange * kTanhRange;
 __device__ __forceinline__ float fmax3(float a, float b, float c) {
   float d;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(d) : "f"(a), "f"(b), "f"(c));
@@ -177,7 +187,8 @@ __device__ __forceinline__ uint64_t exp2_pair(uint64_t x2) {
                __uint_as_float(__float_as_uint(r1) + (__float_as_uint(t1) << 23)));
 }
 
-template <int DH, bool CAP, bool BIAS>
+// CAP: 0 none, 1 up to kShortCap, 2 any.
+template <int DH, int CAP, bool BIAS>
 __global__ void __launch_bounds__(kUmmaThreads, 1)
 umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ CUtensorMap map_k,
             const __grid_constant__ CUtensorMap map_v, const __grid_constant__ CacheAttn p) {
@@ -523,7 +534,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
             for (int x = 0; x < 16; x += 2) {
               uint64_t u;
               float t0, t1, u0, u1;
-              unpack2(tanh_pair(fmul2(pack2(__uint_as_float(s[x]), __uint_as_float(s[x + 1])), pack2(p.scale, p.scale)), u), t0, t1);
+              unpack2(tanh_pair<CAP == 1>(fmul2(pack2(__uint_as_float(s[x]), __uint_as_float(s[x + 1])), pack2(p.scale, p.scale)), u), t0, t1);
               unpack2(u, u0, u1);
               most = fmax3(most, u0, u1);
               s[x] = __float_as_uint(t0);
@@ -536,7 +547,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
               tmem_ld_wait();
 #pragma unroll
               for (int x = 0; x < 16; ++x) {
-                const float t = tanh_fast(__uint_as_float(again[x]) * p.scale);
+                const float t = CAP == 1 ? tanh_far(__uint_as_float(again[x]) * p.scale) : tanh_of(__uint_as_float(again[x]) * p.scale);
                 if (beyond) s[x] = __float_as_uint(t);  // (a row's own way, whatever the others take)
               }
             }
@@ -565,7 +576,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
                 for (int x = 0; x < 16; x += 2) mx = fmax3(mx, __uint_as_float(s[y][x]), __uint_as_float(s[y][x + 1]));
               }
             }
-            if (!BIAS) mx = !CAP ? mx * scale : mx == -INFINITY ? mx : scale * tanh_fast(mx * p.scale);  // (a cap keeps the order)
+            if (!BIAS) mx = !CAP ? mx * scale : mx == -INFINITY ? mx : scale * tanh_of(mx * p.scale);  // (a cap keeps the order)
             *max_own = mx;
             if (!meet(false)) { aborted = true; break; }
             if (m == -INFINITY) m = fmaxf(mx, *max_other);
@@ -793,7 +804,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
   }
 }
 
-template <int DH, bool CAP, bool BIAS>
+template <int DH, int CAP, bool BIAS>
 rocs_status_t launch_umma(const CacheAttn& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int32_t grid,
                           cudaStream_t stream) {
   auto kernel = umma_kernel<DH, CAP, BIAS>;
@@ -803,8 +814,10 @@ rocs_status_t launch_umma(const CacheAttn& p, const CUtensorMap& q, const CUtens
 template <int DH>
 rocs_status_t umma_of(const CacheAttn& p, const CUtensorMap& q, const CUtensorMap& k, const CUtensorMap& v, int32_t grid,
                       cudaStream_t stream) {
-  if (p.cap > 0.f) return p.slopes ? launch_umma<DH, true, true>(p, q, k, v, grid, stream) : launch_umma<DH, true, false>(p, q, k, v, grid, stream);
-  return p.slopes ? launch_umma<DH, false, true>(p, q, k, v, grid, stream) : launch_umma<DH, false, false>(p, q, k, v, grid, stream);
+  const int cap = !(p.cap > 0.f) ? 0 : p.cap <= kShortCap * 1.4426950408889634f ? 1 : 2;  // (p.cap is in log2 units)
+  if (cap == 2) return p.slopes ? launch_umma<DH, 2, true>(p, q, k, v, grid, stream) : launch_umma<DH, 2, false>(p, q, k, v, grid, stream);
+  if (cap == 1) return p.slopes ? launch_umma<DH, 1, true>(p, q, k, v, grid, stream) : launch_umma<DH, 1, false>(p, q, k, v, grid, stream);
+  return p.slopes ? launch_umma<DH, 0, true>(p, q, k, v, grid, stream) : launch_umma<DH, 0, false>(p, q, k, v, grid, stream);
 }
 
 }  // namespace

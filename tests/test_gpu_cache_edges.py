@@ -4,9 +4,14 @@ import torch
 
 import _cache_ref as plain
 from paper_2607_27744_b200 import binding as rocs
-from test_gpu_cache_attention import BF16, bound, build
+from test_gpu_cache_attention import BF16, F32, bound, build, check, slopes
 
 pytestmark = pytest.mark.gpu
+
+# one call for each kernel: (dtype, dh, page, new rows of each request)
+KERNELS = [(BF16, 128, 16, [1, 1, 1]), (BF16, 64, 64, [5, 1, 4]), (BF16, 32, 16, [3, 8, 1]), (BF16, 64, 24, [1, 5, 2]),
+           (BF16, 32, 16, [60, 3, 17]), (BF16, 64, 16, [70, 200, 3]), (BF16, 128, 64, [300, 40, 130]), (BF16, 48, 16, [9, 1, 20]),
+           (F32, 64, 16, [20, 1, 5])]
 
 
 @pytest.mark.parametrize("dh", [64, 128])
@@ -32,3 +37,41 @@ def test_small_tiles_behind_tiles_that_are_computed_again(dh):
         assert bool(((got.double() - O).abs() <= most)[keep].all())
         assert torch.isnan(got[~keep]).all()
     rocs.last_device_status()
+
+
+@pytest.mark.parametrize("dtype,dh,page,counts", KERNELS)
+@pytest.mark.parametrize("cap", [1e3, 1e4, 1e6, 1e9, 1e30])
+@pytest.mark.parametrize("bias", [False, True])
+def test_caps_far_above_the_scores(dtype, dh, page, counts, cap, bias):
+    """A score is right to fp32's roundings of it, however far the cap is above it."""
+    case = build(dtype, counts, [700, 450, 177], 2, 2, dh, page, seed=33)
+    check(case, cap=cap, slopes=slopes(4) if bias else None)
+
+
+@pytest.mark.parametrize("dtype,dh,page,counts", KERNELS)
+@pytest.mark.parametrize("cap", [30.0, 200.0, 1e4])
+def test_scores_of_hundreds_under_a_cap(dtype, dh, page, counts, cap):
+    check(build(dtype, counts, [700, 450, 177], 2, 2, dh, page, seed=34, std=40.0), cap=cap)
+
+
+@pytest.mark.parametrize("dtype,dh,page,counts", KERNELS)
+@pytest.mark.parametrize("cap", [50.0, 1e4, 1e6, 1e9])
+def test_one_score_beyond_the_cap_below_all_others(dtype, dh, page, counts, cap):
+    """Keys whose scores end at -cap, and weigh nothing, beside others whose scores are far from it: how far those may be off goes
+    by their own size."""
+    lens = [700, 450, 177]
+    case = build(dtype, counts, lens, 2, 2, dh, page, seed=35)
+    case["K"][..., 0] = torch.where(case["K"][..., 0].isnan(), case["K"][..., 0], 0.0)
+    case["Q"][..., 0] = 8.0
+    _, _, S = plain.attention(case["K"], case["V"], case["table"], case["lens"], case["offsets"], case["Q"], case["slots"].tolist(), scale=0.125)
+    for r in range(3):
+        for j in (3, 40, 100):
+            row = case["table"][case["slots"][r].long()]
+            case["K"][int(row[j // page]), j % page, :, 0] = -2.0 * cap
+    O, A, _ = plain.attention(case["K"], case["V"], case["table"], case["lens"], case["offsets"], case["Q"], case["slots"].tolist(),
+                              scale=0.125, cap=cap)
+    got = rocs.cache_attention(rocs.cache_create(case["K"], case["V"], case["table"], case["lens"]), case["plan"], case["Q"],
+                               slots=case["slots"], scale=0.125, cap=cap)
+    off = (got.double() - O).abs()
+    most = bound(dtype, O, A, S, 700, dh)
+    assert bool((off <= most).all()), f"off by {float((off / most).max()):.3f} of the bound"
