@@ -374,7 +374,8 @@ rocs_status_t rocs_cache_compact(const rocs_cache_t* cache, int32_t* table_out, 
  *   begin [N] int32 or NULL: row i sees no key in front of begin[i] (the start of its session or document)
  *   prefix [R] int32 or NULL: keys in front of prefix[r] are visible to all of r's rows
  *   score  x_j = scale <q, k_j>, scale <= 0: 1/sqrt(dh);  cap > 0: x_j = cap tanh(x_j / cap);  slopes [H] fp32 or NULL:
- *          x_j - slopes[h] |p - j|  (scale / ln 2 and scale / cap finite in fp32)
+ *          x_j - slopes[h] |p - j|.  In fp32 scale / ln 2, cap / ln 2 and scale / cap are finite, the last not below 2^-126; a cap
+ *          of 2^64 or more with which it is below that counts as none
  *   O[i, h, :] = sum_j softmax_j(x) V_j over the visible j, zeros where none is.  H query heads, a multiple of the cache's
  *   H_kv: head h reads key head h / (H / H_kv).
  *   Q [N, H, dh], ld_qt, ld_qh and O [N, H, dh], ld_ot, ld_oh: strides of row and head (elements, of 16-byte multiples)

@@ -2,6 +2,7 @@
 // kernel (fp32, head dimensions that the tensor-core kernels do not take).
 #include <algorithm>
 #include <cmath>
+#include <limits>
 
 #include "cache_attn.cuh"
 
@@ -527,6 +528,14 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
   if (H > 65535) return ROCS_ERR_UNSUPPORTED;
   if (!(scale > 0.f)) scale = 1.0f / sqrtf((float)c->dh);
   if (!std::isfinite(scale * kLog2e) || (cap > 0.f && !std::isfinite(scale / cap))) return ROCS_ERR_INVALID_ARG;
+  if (cap > 0.f && scale / cap < std::numeric_limits<float>::min()) {
+    // The kernels' factor would lose bits, or be 0.  Products of fp32 stay below 2^128, so that no score is above 4 caps.  One
+    // below 2^-12 of the cap is, to 2^-25 of it, what it is without a cap; if the cap is 2^64 at least, others are 2^28 apart, or
+    // equal, in fp32, and under the cap still 2^18: the largest has all the weight either way.
+    if (cap < 0x1p64f) return ROCS_ERR_INVALID_ARG;
+    cap = 0.f;
+  }
+  if (!std::isfinite(cap * kLog2e)) return ROCS_ERR_INVALID_ARG;
   const Choice x = choose(c, plan, H, kernel_path(), (H == 1 || ld_qh > 0) && (plan->N == 1 || ld_qt > 0));
   const Places w = places(x, c->dh);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || bytes < w.bytes) return ROCS_ERR_WORKSPACE;

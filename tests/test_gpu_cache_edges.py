@@ -75,3 +75,17 @@ def test_one_score_beyond_the_cap_below_all_others(dtype, dh, page, counts, cap)
     off = (got.double() - O).abs()
     most = bound(dtype, O, A, S, 700, dh)
     assert bool((off <= most).all()), f"off by {float((off / most).max()):.3f} of the bound"
+
+
+@pytest.mark.parametrize("dtype,dh,page,counts", KERNELS)
+@pytest.mark.parametrize("cap", [1e37, 3e38, torch.finfo(F32).max])
+def test_caps_at_the_end_of_what_fp32_holds(dtype, dh, page, counts, cap):
+    case = build(dtype, counts, [700, 450, 177], 2, 2, dh, page, seed=38)
+    check(case, cap=cap)
+    cache = rocs.cache_create(case["K"], case["V"], case["table"], case["lens"])
+    out = torch.full_like(case["Q"], 7.0)
+    for how in (dict(cap=3e38, scale=4.0), dict(cap=10.0, scale=1e-38), dict(cap=1e19, scale=1e-30)):
+        with pytest.raises(rocs.RocsError, match="invalid"):
+            rocs.cache_attention(cache, case["plan"], case["Q"], slots=case["slots"], out=out, **how)
+    torch.cuda.synchronize()
+    assert torch.all(out == 7.0)
