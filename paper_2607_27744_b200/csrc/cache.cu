@@ -174,18 +174,18 @@ extend_kernel(CacheBooks c, const int32_t* slots, const int32_t* off, int32_t R,
     const int32_t at = block_prefix(need, sum);
     if (r < R) {
       if (near) {
-        near_before[r] = (int32_t)total64 + at;
+        near_before[r] = (int32_t)(total64 + at);
         near_place[r] = my_start;
       } else {
-        b.before[r] = (int32_t)total64 + at;
+        b.before[r] = (int32_t)(total64 + at);
         b.start[r] = my_start;
       }
     }
     total64 += sum;
-    if (total64 > c.n_pages) total64 = (int64_t)c.n_pages + 1;  // more than there are, whatever comes: refused below
   }
-  const int32_t total = (int32_t)total64;
-  // that many free pages, lowest first
+  // That many free pages, lowest first.  (What the call needs may be beyond the pool and beyond 32 bits: then all free ones are
+  // counted, and nothing is dealt out.)
+  const int32_t total = (int32_t)min(total64, (int64_t)c.n_pages + 1);
   int32_t found = 0;
   for (int32_t p0 = 0; p0 < c.n_pages && found < total; p0 += 4 * kBookThreads) {
     const int32_t p = p0 + 4 * (int32_t)threadIdx.x;
@@ -209,7 +209,7 @@ extend_kernel(CacheBooks c, const int32_t* slots, const int32_t* off, int32_t R,
     b.head[0] = status;
     if (report) {
       report[0] = status;
-      report[1] = ok ? total : status == kFewPages ? total - found : 0;
+      report[1] = ok ? total : status == kFewPages ? (int32_t)min(total64 - found, (int64_t)0x7fffffff) : 0;
     }
   }
   if (!ok) {

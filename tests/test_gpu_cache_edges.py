@@ -5,6 +5,7 @@ import torch
 import _cache_ref as plain
 from paper_2607_27744_b200 import binding as rocs
 from test_gpu_cache_attention import BF16, F32, bound, build, check, slopes
+from test_gpu_cache_books import Pair, ints, plan_of
 
 pytestmark = pytest.mark.gpu
 
@@ -89,3 +90,21 @@ def test_caps_at_the_end_of_what_fp32_holds(dtype, dh, page, counts, cap):
             rocs.cache_attention(cache, case["plan"], case["Q"], slots=case["slots"], out=out, **how)
     torch.cuda.synchronize()
     assert torch.all(out == 7.0)
+
+
+@pytest.mark.parametrize("n_pages,n_slots,width,n", [(10, 3, 40, 40), (5000, 5, 2000, 2000), (10, 1500, 2, 1), (4097, 1500, 4, 4), (9000, 3, 4000, 4000)])
+def test_how_many_pages_are_missing(n_pages, n_slots, width, n):
+    pair = Pair(BF16, 1, n_pages, 1, 1, 8, n_slots + 1, width)
+    pair.extend([n_slots], [2])
+    pair.extend(list(range(n_slots)), [n] * n_slots)
+    assert pair.report.tolist() == [1, n * n_slots - (n_pages - 2)]
+
+
+def test_nearly_as_many_pages_are_missing_as_rows_can_be_named():
+    pair = Pair(BF16, 1, 10, 1, 1, 8, 2047, 1)
+    wide = torch.full((2047, 1 << 20), -1, dtype=torch.int32, device="cuda")
+    cache = rocs.cache_create(pair.K, pair.V, wide, pair.lens, pair.refs)
+    off = torch.arange(2048, dtype=torch.int32) * (1 << 20)
+    first = rocs.cache_extend(cache, rocs.plan_create(off.cuda(), off), report=pair.report)
+    assert pair.report.tolist() == [1, 2047 * (1 << 20) - 10] and bool((first == -1).all())
+    assert bool((pair.lens == 0).all()) and bool((pair.refs == 0).all())
