@@ -347,6 +347,12 @@ __global__ void __launch_bounds__(kGenThreads) general_kernel(const CacheAttn p)
         pr[i] = s[i] == -INFINITY ? 0.f : exp2f((s[i] - m[i]) * kLog2e);
         l[i] += pr[i];
       }
+      // a key that a row does not see adds nothing, whatever its value holds; one that it sees does, whatever its weight
+      if (!full) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (j < keys[i].lo || j >= keys[i].hi) pr[i] = -1.f;
+      }
       *reinterpret_cast<float4*>(probs[warp][lane]) = make_float4(pr[0], pr[1], pr[2], pr[3]);
       __syncwarp();
       auto add_values = [&](bool masked) {
@@ -361,11 +367,10 @@ __global__ void __launch_bounds__(kGenThreads) general_kernel(const CacheAttn p)
             float x;
             if constexpr (sizeof(T) == 4) x = reinterpret_cast<const float*>(vr)[d];
             else x = __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(vr)[d]);
-            // a key that a row does not see adds nothing, whatever its value holds
-            if (!masked || w.x != 0.f) acc[0][c] = fmaf(w.x, x, acc[0][c]);
-            if (!masked || w.y != 0.f) acc[1][c] = fmaf(w.y, x, acc[1][c]);
-            if (!masked || w.z != 0.f) acc[2][c] = fmaf(w.z, x, acc[2][c]);
-            if (!masked || w.w != 0.f) acc[3][c] = fmaf(w.w, x, acc[3][c]);
+            if (!masked || !(w.x < 0.f)) acc[0][c] = fmaf(w.x, x, acc[0][c]);
+            if (!masked || !(w.y < 0.f)) acc[1][c] = fmaf(w.y, x, acc[1][c]);
+            if (!masked || !(w.z < 0.f)) acc[2][c] = fmaf(w.z, x, acc[2][c]);
+            if (!masked || !(w.w < 0.f)) acc[3][c] = fmaf(w.w, x, acc[3][c]);
           }
         }
       };

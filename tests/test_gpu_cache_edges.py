@@ -108,3 +108,24 @@ def test_nearly_as_many_pages_are_missing_as_rows_can_be_named():
     first = rocs.cache_extend(cache, rocs.plan_create(off.cuda(), off), report=pair.report)
     assert pair.report.tolist() == [1, 2047 * (1 << 20) - 10] and bool((first == -1).all())
     assert bool((pair.lens == 0).all()) and bool((pair.refs == 0).all())
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf")])
+@pytest.mark.parametrize("dtype,dh,page,counts", KERNELS)
+def test_a_key_that_weighs_nothing_but_is_seen(dtype, dh, page, counts, value):
+    """exp of a score far below the others is 0 in fp32, and 0 x NaN or Inf is NaN: whatever masks the block and its other rows have."""
+    lens = [700, 450, 177]
+    case = build(dtype, counts, lens, 1, 2, dh, page, seed=36)
+    case["K"][..., 0] = torch.where(case["K"][..., 0].isnan(), case["K"][..., 0], 0.0)
+    case["Q"][..., 0] = 8.0
+    sees = torch.zeros(case["offsets"][-1], dtype=torch.bool)
+    for r, (n, L) in enumerate(zip(counts, lens)):
+        j = L - 1 - n // 2
+        row = case["table"][case["slots"][r].long()]
+        case["K"][int(row[j // page]), j % page, :, 0] = -1e6
+        case["V"][int(row[j // page]), j % page] = value
+        sees[case["offsets"][r] + n - 1 - n // 2:case["offsets"][r + 1]] = True
+    got = rocs.cache_attention(rocs.cache_create(case["K"], case["V"], case["table"], case["lens"]), case["plan"], case["Q"],
+                               slots=case["slots"], scale=0.125)
+    assert not torch.isfinite(got[sees.cuda()]).any()
+    assert torch.isfinite(got[~sees.cuda()]).all()
