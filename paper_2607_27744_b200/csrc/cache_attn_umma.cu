@@ -502,7 +502,8 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
         if (i >= first + 2 * step) {
           const float most = fmaxf(own[cnt_s & 1], sum_other[((cnt_s - 2) & 3) * 4 * kSide]);
           // (as long as the reference moved for the block in front of it, its sum was that of the old one)
-          if (most > kMoveAt * moved) up = (float)((int32_t)(__float_as_uint(most / moved) >> 23) - 127);
+          // (and by what fp32 lets it: scores of 2^24 and more are further apart than 1)
+          if (most > kMoveAt * moved) up = rintf((m + (float)((int32_t)(__float_as_uint(most / moved) >> 23) - 127)) - m);
         }
         const bool slow = __any_sync(0xffffffffu, m == -INFINITY || up != 0.f);
         if (!mbar_wait_suspended(sb + C::kSFull + 8 * side, cnt_s & 1, abort_flag, p.status, kStatusCache | 10)) { aborted = true; break; }

@@ -129,3 +129,29 @@ def test_a_key_that_weighs_nothing_but_is_seen(dtype, dh, page, counts, value):
                                slots=case["slots"], scale=0.125)
     assert not torch.isfinite(got[sees.cuda()]).any()
     assert torch.isfinite(got[~sees.cuda()]).all()
+
+
+@pytest.mark.parametrize("dtype,dh,page,counts", KERNELS)
+@pytest.mark.parametrize("base", [2.0 ** 10, 2.0 ** 24, 2.0 ** 26, 2.0 ** 28])
+@pytest.mark.parametrize("causal", [True, False])
+def test_large_scores_that_pass_the_first_keys_by_little(dtype, dh, page, counts, base, causal):
+    """Exact scores of `base`, and of 32 more for every 50th key but the last 500: the result is the mean over those.  A reference
+    found in the last keys has to move by 46 powers of two, which fp32 cannot add to numbers of this size."""
+    lens = [1700, 1450, 977]
+    case = build(dtype, counts, lens, 40, 2, dh, page, seed=39)   # (heads enough for pieces of many blocks)
+    case["Q"].zero_()
+    case["Q"][..., 0] = 2.0 ** 10
+    case["Q"][..., 1] = 8.0
+    case["K"][..., :2] = torch.where(case["K"][..., :2].isnan(), case["K"][..., :2], 0.0)
+    case["K"][..., 0] += base / 2.0 ** 10
+    for r, L in enumerate(lens):
+        row = case["table"][case["slots"][r].long()]
+        for j in range(0, L - 500, 50):
+            case["K"][int(row[j // page]), j % page, :, 1] = 4.0
+    got = rocs.cache_attention(rocs.cache_create(case["K"], case["V"], case["table"], case["lens"]), case["plan"], case["Q"],
+                               slots=case["slots"], scale=1.0, causal=causal)
+    O, A, S = plain.attention(case["K"], case["V"], case["table"], case["lens"], case["offsets"], case["Q"], case["slots"].tolist(),
+                              scale=1.0, causal=causal)
+    # (the other keys' weights are e^-32 each, of a sum of ten and more: their errors are far below a rounding)
+    off, most = (got.double() - O).abs(), bound(dtype, O, A, torch.zeros_like(S), 1700, dh)
+    assert bool((off <= most).all()), f"off by {float((off / most).max()):.3f} of the bound"
