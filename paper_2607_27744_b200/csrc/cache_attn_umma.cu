@@ -491,7 +491,8 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       const int32_t blk0 = e.blk0 + walk.block0(p), n = walk.blocks(p);
       const int32_t step = split ? 2 : 1, first = split ? side : 0;
       // -inf: no reference yet.  Capped scores need none, unless the cap is beyond what fp32's range has room for.
-      float m = sees && !(CAP && !BIAS && p.cap <= 80.f) ? -INFINITY : 0.f, l = 0.f;
+      const bool bounded = CAP && !BIAS && p.cap <= 80.f;
+      float m = sees && !bounded ? -INFINITY : 0.f, l = 0.f;
       float own[2] = {0.f, 0.f};  // this half's sums of the last two blocks
       float moved = 1.f;          // 2^(what the reference moved by for the last block)
       bool aborted = false;
@@ -768,9 +769,10 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       if (leads) {
         bad = there && (split ? ends[0].z + ends[kSide].z + ends[2 * kSide].z + ends[3 * kSide].z
                               : ends[side * 2 * kSide].z + ends[(side * 2 + 1) * kSide].z) != 0.f;
-        // Scores of 2^31 and more: their product with the scale is not rounded where the reference was, so that all weights may
-        // have come out as 0.
-        bad = bad || (sees && l_all == 0.f && keys.lo < (blk0 + n) * BK && keys.hi > blk0 * BK);
+        // Scores of 2^30 and more: their product with the scale is not rounded where the reference was, so that the largest weight
+        // may have come out as 2^-64 and less, beside others that 2^-126 or exp2_pair's least cut off.  (Without a reference it may
+        // be 2^-80.)
+        bad = bad || (sees && l_all < (bounded ? 0x1p-100f : 0x1p-64f) && keys.lo < (blk0 + n) * BK && keys.hi > blk0 * BK);
       }
       uint32_t redo = __ballot_sync(0xffffffffu, bad);
       while (redo != 0) {  // a row at a time, by the warp

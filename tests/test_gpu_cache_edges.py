@@ -155,3 +155,29 @@ def test_large_scores_that_pass_the_first_keys_by_little(dtype, dh, page, counts
     # (the other keys' weights are e^-32 each, of a sum of ten and more: their errors are far below a rounding)
     off, most = (got.double() - O).abs(), bound(dtype, O, A, torch.zeros_like(S), 1700, dh)
     assert bool((off <= most).all()), f"off by {float((off / most).max()):.3f} of the bound"
+
+
+@pytest.mark.parametrize("dtype,dh,page,counts", KERNELS)
+@pytest.mark.parametrize("size", [2.0 ** 28, 1.5 * 2.0 ** 30, 2.0 ** 31, 1.25 * 2.0 ** 33, 1.5 * 2.0 ** 40])
+@pytest.mark.parametrize("top", [False, True])
+@pytest.mark.parametrize("heads", [1, 40])   # pieces of one block, or of many
+def test_scores_beyond_32_bits(dtype, dh, page, counts, size, top, heads):
+    """Scores so large that fp32's next one is 2^5 to 2^17 away: all equal (products of powers of two and 3 or 5, exact), or one
+    above the others; the mean of the values, or the one's."""
+    lens = [1700, 1450, 977]
+    case = build(dtype, counts, lens, heads, 2, dh, page, seed=37)
+    case["Q"].zero_()
+    case["Q"][..., 0] = 2.0 ** 10
+    case["K"][..., 0] = torch.where(case["K"][..., 0].isnan(), case["K"][..., 0], size / 2.0 ** 10)
+    if top:
+        for r in range(3):
+            row = case["table"][case["slots"][r].long()]
+            case["K"][int(row[600 // page]), 600 % page, :, 0] *= 1.03125
+    for scale in (0.11, 0.3, 0.7, 0.9, 1.3, 3.3) if heads == 1 else (0.7, 1.3):
+        for causal in (True, False) if heads == 1 else (True,):
+            got = rocs.cache_attention(rocs.cache_create(case["K"], case["V"], case["table"], case["lens"]), case["plan"], case["Q"],
+                                       slots=case["slots"], scale=scale, causal=causal)
+            O, A, S = plain.attention(case["K"], case["V"], case["table"], case["lens"], case["offsets"], case["Q"],
+                                      case["slots"].tolist(), scale=scale, causal=causal)
+            off, most = (got.double() - O).abs(), bound(dtype, O, A, torch.zeros_like(S), 1700, dh)
+            assert bool((off <= most).all()), (scale, causal, f"off by {float((off / most).max()):.3f} of the bound")
