@@ -1,4 +1,6 @@
 """The paged cache where one tile, one row or one call leaves something to the next."""
+import random
+
 import pytest
 import torch
 
@@ -181,3 +183,37 @@ def test_scores_beyond_32_bits(dtype, dh, page, counts, size, top, heads):
                                       case["slots"].tolist(), scale=scale, causal=causal)
             off, most = (got.double() - O).abs(), bound(dtype, O, A, torch.zeros_like(S), 1700, dh)
             assert bool((off <= most).all()), (scale, causal, f"off by {float((off / most).max()):.3f} of the bound")
+
+
+def test_more_free_pages_than_are_kept_near():
+    """Calls that take more than 4096 pages, found between held ones and beyond the first 4096 of the pool."""
+    rng = random.Random(6)
+    pair = Pair(BF16, 1, 14000, 1, 1, 8, 2000, 40)
+    pair.extend(list(range(100)), [30] * 100)
+    pair.truncate(list(range(0, 100, 2)), [rng.randint(0, 20) for _ in range(50)])
+
+    def grow(slots, counts):
+        status, pages, first, copies = pair.books.extend(slots, counts)
+        got = rocs.cache_extend(pair.cache, plan_of(counts), slots=ints(slots), report=pair.report)
+        assert got.tolist() == first
+        pair.check(status, pages)
+
+    grow(list(range(100, 400)), [rng.randint(15, 25) for _ in range(300)])
+    pair.truncate(list(range(100, 400, 3)))
+    grow(list(range(400, 1900)), [rng.randint(0, 6) for _ in range(1500)])
+
+
+def test_more_slots_than_a_block_has_bits_for():
+    """Above 262144 slots a slot named twice is found by a word in the workspace."""
+    n = 32 * 8192 + 100
+    pair = Pair(BF16, 1, 50, 4, 1, 8, n, 2)
+    pair.extend([n - 1, 5, n - 60, 0], [6, 3, 8, 1])
+    pair.extend([n - 1, 7, n - 1], [1, 1, 1])
+    assert pair.report.tolist() == [2, 0]
+    pair.fork([n - 60, n - 1], [9, 100000])
+    pair.fork([5, 5], [n - 2, n - 2])
+    pair.extend([n - 1, 100000], [1, 1])
+    pair.truncate([n - 1, 9, n - 1])
+    assert pair.report.tolist() == [2, 0]
+    pair.truncate([n - 1, 9, 5], [4, 0, 0])
+    pair.compact()
