@@ -310,14 +310,16 @@ rocs_status_t rocs_linear_normed(rocs_dtype_t dtype, rocs_norm_t kind, int64_t M
  * A cache names these arrays (16-byte aligned, device memory of the caller, who may read and write them in stream
  * order) and owns no device memory; creating and destroying it enqueues nothing.  Lengths outside 0..width * page count
  * as the nearer end.  An entry of the table outside 0..n_pages-1 reads as a page of zeros and is never written through.
- * Limits: width <= 2^20, width * page <= 2^30, page * H_kv * dh < 2^31, dh <= 256, dh * sizeof(element) a multiple of 16.
+ * Limits: width <= 2^20, width * page <= 2^30, page * H_kv * dh < 2^31, dh <= 256, dh * sizeof(element) a multiple of 16;
+ * n_pages, n_slots and the slots of a call < 2^31 - 2^13.
  *
  * The calls that keep the books (extend, fork, truncate, compact) run on the device without the host: no
  * synchronisation, and a captured one works on what it finds at each replay.  They are all or nothing: a call that
  * cannot be carried out changes nothing and says so in `report` (device int32 [2], may be NULL): [0] 0 = done,
  * 1 = too few free pages, 2 = a slot out of range or named twice, 3 = a slot would outgrow its row of the table or has a
- * length outside it, 4 = a child that is not empty, 5 = a page id outside the pool; [1] pages taken / shared / given
- * back / in use (extend / fork / truncate / compact; for 1 how many are missing).  `workspace`: rocs_cache_workspace
+ * length outside it, or more than 2^30 entries in all to fork or truncate, 4 = a child that is not empty, 5 = a page id
+ * outside the pool; [1] pages taken / shared / given back / in use (extend / fork / truncate / compact; for 1 how many are
+ * missing).  `workspace`: rocs_cache_workspace
  * bytes for the largest number of slots of a call, 256-byte aligned, contents overwritten.
  * Errors of all: INVALID_ARG, ALIGNMENT, WORKSPACE, UNSUPPORTED, CUDA.
  */

@@ -554,6 +554,7 @@ PageShape page_shape(const rocs_cache* c) {
 
 rocs_status_t check_books(const rocs_cache* c, int32_t n, const void* workspace, size_t bytes) {
   if (!c || n < 0 || !c->refs) return ROCS_ERR_INVALID_ARG;
+  if (n > kMostCounted) return ROCS_ERR_UNSUPPORTED;
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || bytes < rocs_cache_workspace(c, n)) return ROCS_ERR_WORKSPACE;
   return ROCS_OK;
 }
@@ -602,7 +603,8 @@ rocs_status_t rocs_cache_create(rocs_cache_t** out, rocs_dtype_t dtype, int32_t 
       span += (d.n - 1) * *d.ld;
     }
   // (width: prefix sums over 1024 rows of the table stay in 32 bits; positions: so does the next multiple of a block or a page)
-  if (dh > 256 || (int64_t)width * page > (1ll << 30) || width > (1 << 20) || (int64_t)page * H_kv * dh > 0x7fffffffLL)
+  if (dh > 256 || (int64_t)width * page > (1ll << 30) || width > (1 << 20) || (int64_t)page * H_kv * dh > 0x7fffffffLL ||
+      n_pages > kMostCounted || n_slots > kMostCounted)
     return ROCS_ERR_UNSUPPORTED;
   rocs_cache* c = new (std::nothrow) rocs_cache{dtype, layers, n_pages, page, H_kv, dh, K, V, ld_layer, ld_page, ld_token, ld_head,
                                                 n_slots, width, table, lens, refs};

@@ -17,6 +17,9 @@ namespace rocs {
 
 int kernel_path();  // of rocs_set_path
 
+// Pages, slots, and slots or tiles of a call at most: a block that goes over them some thousands at a time ends in 32 bits.
+constexpr int32_t kMostCounted = 0x7fffffff - 8192;
+
 // SMs of the current device, asked for once per device.
 inline int sms_of_device() {
   static std::atomic<int> known[64];

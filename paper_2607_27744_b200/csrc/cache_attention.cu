@@ -544,7 +544,7 @@ rocs_status_t rocs_cache_attention(const rocs_cache_t* c, int32_t layer, const r
   const Choice x = choose(c, plan, H, kernel_path(), (H == 1 || ld_qh > 0) && (plan->N == 1 || ld_qt > 0));
   const Places w = places(x, c->dh);
   if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255u) || bytes < w.bytes) return ROCS_ERR_WORKSPACE;
-  if (x.entries > 0x7fffffffLL) return ROCS_ERR_UNSUPPORTED;
+  if (x.entries > kMostCounted) return ROCS_ERR_UNSUPPORTED;
   cudaStream_t stream = (cudaStream_t)stream_;
   CacheAttn p{};
   p.K = static_cast<const uint8_t*>(c->K) + layer * c->ld_layer * es;

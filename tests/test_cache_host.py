@@ -114,3 +114,20 @@ def test_the_binding_takes_tensors_of_the_gpu_only():
                  lambda: binding.cache_extend(closed, plan), lambda: binding.cache_append(closed, plan, n, K, K)):
         with pytest.raises(ValueError, match="closed"):
             call()
+
+
+def test_how_many_pages_and_slots_are_counted(lib):
+    """Kernels go over pages and slots some thousands at a time, in 32 bits."""
+    most = (1 << 31) - (1 << 13) - 1
+    for name in ("n_pages", "n_slots"):
+        small = dict(page=1, H=1, layers=1, dh=8, ld_head=0, ld_token=0, ld_page=8, ld_layer=0)
+        got, handle = create(lib, **small, **{name: most})
+        assert got == 0
+        lib.rocs_cache_destroy(handle)
+        got, handle = create(lib, **small, **{name: most + 1})
+        assert got == UNSUPPORTED and not handle
+    _, c = create(lib)
+    for n in (most + 1, (1 << 31) - 1):
+        assert lib.rocs_cache_fork(c, n, P, P, None, P, 1 << 40, None) == UNSUPPORTED
+        assert lib.rocs_cache_truncate(c, n, P, None, None, P, 1 << 40, None) == UNSUPPORTED
+    lib.rocs_cache_destroy(c)
