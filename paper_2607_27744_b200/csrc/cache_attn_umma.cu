@@ -166,6 +166,11 @@ __device__ __forceinline__ void transpose_pieces(uint4 (&v)[4], int lane) {
   swap_pieces(v[1], v[3], lane & 2, 2);
 }
 
+// 2^-n for n >= 0, with the denormal numbers below 2^-126.
+__device__ __forceinline__ float exp2_down(int32_t n) {
+  return __uint_as_float(n < 127 ? (uint32_t)(127 - n) << 23 : n < 150 ? 1u << (149 - n) : 0u);
+}
+
 // 2^x for a pair on the FMA pipes: 2^n 2^f with n the nearest integer and a polynomial of degree 3 for 2^f on [-1/2, 1/2]
 // (fitted for the least relative error, 7.5e-5: a 26th of the rounding to bf16 that follows).  Below 2^-125 it stays there;
 // what is NaN, or too large for fp32, comes out as NaN, or so large that bf16 has an infinity for it.
@@ -584,7 +589,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
             if (m == -INFINITY) m = fmaxf(mx, *max_other);
           }
           if (__any_sync(0xffffffffu, up != 0.f)) {
-            const float a = __uint_as_float((uint32_t)max(127 - (int32_t)up, 0) << 23);  // 2^-up
+            const float a = exp2_down((int32_t)up);
             m += up;
             l *= a;
 #pragma unroll 1
@@ -685,8 +690,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
         if (both) {
           m_all = fmaxf(a0.x, b0.x);
           const float r = m_all == -INFINITY ? 0.f : m_all;
-          wa = ex2_approx(a0.x - r);
-          wb = ex2_approx(b0.x - r);
+          // (denormal weights count: the sums beside them may be up to 2^128)
+          wa = exp2f(a0.x - r);
+          wb = exp2f(b0.x - r);
           l_all = wa * l_all + wb * (b0.y + b1.y);
         }
       } else {
@@ -694,7 +700,14 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       }
       const bool whole = walk.whole();
       const int32_t part = walk.part();
-      const float inv = whole ? (sees ? 1.f / l_all : 0.f) : 1.f;
+      float inv = whole ? (sees ? 1.f / l_all : 0.f) : 1.f;
+      const bool beyond = !(l_all < INFINITY);
+      if (!whole && l_all > 0x1p64f) {  // the reference is where the sum is, so that sums of parts stay in fp32's range
+        const float by = rintf((m_all + (float)((int32_t)(__float_as_uint(l_all) >> 23) - 127)) - m_all);
+        inv = exp2_down((int32_t)by);
+        m_all += by;
+        l_all *= inv;
+      }
       // non-finite, or only scores of -inf, which exp2_pair does not take to 0: by hand
       float probe = m == -INFINITY && l != 0.f ? NAN : l * 0.f;
       float* to = attn_part(p, part) + (int64_t)tile_row * DH + col0;
@@ -705,13 +718,9 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       for (int k = 0; k < 4; ++k)
         out4[k] = reinterpret_cast<uint8_t*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(out), lane0 + k));
       auto column = [&](uint32_t a, uint32_t b) {  // of the row's result
-        float v = __uint_as_float(a);
+        float v = __uint_as_float(a) * wa;
+        if (both) v = fmaf(__uint_as_float(b), wb, v);
         probe = fmaf(v, 0.f, probe);
-        v *= wa;
-        if (both) {
-          probe = fmaf(__uint_as_float(b), 0.f, probe);
-          v = fmaf(__uint_as_float(b), wb, v);
-        }
         return v * inv;
       };
 #pragma unroll 1
@@ -772,6 +781,7 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
         // Scores of 2^30 and more: their product with the scale is not rounded where the reference was, so that the largest weight
         // may have come out as 2^-64 and less, beside others that 2^-126 or exp2_pair's least cut off.  (Without a reference it may
         // be 2^-80.)
+        bad = bad || (there && beyond);
         bad = bad || (sees && l_all < (bounded ? 0x1p-100f : 0x1p-64f) && keys.lo < (blk0 + n) * BK && keys.hi > blk0 * BK);
       }
       uint32_t redo = __ballot_sync(0xffffffffu, bad);

@@ -185,6 +185,32 @@ def test_scores_beyond_32_bits(dtype, dh, page, counts, size, top, heads):
             assert bool((off <= most).all()), (scale, causal, f"off by {float((off / most).max()):.3f} of the bound")
 
 
+@pytest.mark.parametrize("dtype,dh,page,counts", KERNELS)
+@pytest.mark.parametrize("heads", [1, 24])
+@pytest.mark.parametrize("seed", range(6))
+def test_scores_that_pass_the_first_keys_by_all_of_fp32s_exponents(dtype, dh, page, counts, heads, seed):
+    """Scores of 0, and here and there, but not among the last keys, of 87 to 95: their weights relative to the last keys' are at the
+    end of fp32's range or beyond it, in one block or on one side of a tile and nearly as large on the other.  (Values are
+    small, so that weights of 2^127 times values have a place in fp32.)"""
+    rng = random.Random(seed)
+    lens = [1700, 1450, 977]
+    case = build(dtype, counts, lens, heads, 2, dh, page, seed=40 + seed)
+    case["V"] *= 0.125
+    case["Q"].zero_()
+    case["Q"][..., 0] = 1.0
+    case["K"][..., 0] = torch.where(case["K"][..., 0].isnan(), case["K"][..., 0], 0.0)
+    for r, L in enumerate(lens):
+        row = case["table"][case["slots"][r].long()]
+        last = L // 128 * 128
+        some = rng.sample(range(last), 8) if seed < 3 else [rng.randrange(last - 128, last), rng.randrange(last - 256, last - 128),
+                                                            rng.randrange(last - 384, last - 256)]
+        for j in some:
+            score = rng.choice([88.0, 88.25] if seed < 2 else [87.5, 88.25, 88.5, 95.0]) if seed < 3 else 88.5 if j >= last - 128 else 87.5
+            case["K"][int(row[j // page]), j % page, :, 0] = score
+    for causal in (True, False):
+        check(case, scale=1.0, causal=causal)
+
+
 def test_more_free_pages_than_are_kept_near():
     """Calls that take more than 4096 pages, found between held ones and beyond the first 4096 of the pool."""
     rng = random.Random(6)
