@@ -562,7 +562,7 @@ rocs_status_t check_books(const rocs_cache* c, int32_t n, const void* workspace,
 size_t claim_bytes(const rocs_cache* c) { return c->n_slots <= kBitSlots ? sizeof(uint32_t) * (size_t)((c->n_slots + 31) / 32) : 0; }
 
 // How many CTAs copy: several rounds of the chip, so that it is busy to the end (7143 pages, two thirds in use, 6 layers: 239 us
-// with 4 per SM, 229 us with 8), fewer where the pool could not give them a piece each.
+// with 4 per SM, 229 us with 8, 215 us with 16), fewer where the pool could not give them a piece each.
 unsigned copy_grid(const rocs_cache* c, const PageShape& g, int64_t most_pairs, int64_t entries) {
   const int64_t chunks = ((int64_t)g.outer * g.inner * g.vecs + kChunk - 1) / kChunk;
   const int64_t want = std::max(most_pairs * c->layers * 2 * chunks, (entries + kCopyThreads - 1) / kCopyThreads);

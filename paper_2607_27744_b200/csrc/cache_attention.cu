@@ -449,6 +449,9 @@ Choice choose(const rocs_cache* c, const rocs_plan* plan, int32_t H, int path, b
     // 18.8 / 20.2 / 21.8 / 20.0 and 12.2 / 14.2 / 17.2 / 18.6 / 18.7 us; 24 requests over 1000 keys, 8 heads of 64: 40 / 64 / 100
     // rows 28.3 / 28.7 / 29.8 and 28.7 / 32.3 / 47.9; 8 over 2000, 8 heads of 128: 40 / 64 / 100 rows 26.9 / 27.9 / 30.2 and 34.8 /
     // 37.6 / 58.8.  How many keys there are is known on the device only; the table's width says how many there may be.
+    // A batch of a chunk and single events goes the chunk's way, all of it: 300 rows over 4000 keys beside 48 events over 500-8000,
+    // 8 heads of 64, 77 us, and 99 us as a call for the chunk (35) and one for the events (65); 8 x 4 heads of 128 130 and 154 us;
+    // 40 rows beside 64 events, 8 heads of 64, 99 and 113 us.
     const bool many_keys = (int64_t)c->width * c->page >= 512;
     // (its tensor map of Q takes no stride of 0)
     if (q_spread && (int64_t)plan->largest * g > (many_keys ? 32 : 128) && attn_umma_supported(c->dh, c->page)) {

@@ -11,6 +11,8 @@
 //
 // Every warp keeps a reference and sums of its own per row; the reference moves when a score passes it by 2^8, which one vote
 // per block asks for.  At the end of a piece the four add up through shared memory.
+// Probabilities are rounded to bf16 as the second product's operand (half a step, 2^-9 to 2^-8 of each; the plain form does not:
+// errors of 2.3e-3 and 1.7e-3 of the values against 64 bits, the result's own rounding among them); their sum is of unrounded ones.
 #include <algorithm>
 
 #include "cache_attn.cuh"

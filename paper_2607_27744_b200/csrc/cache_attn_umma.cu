@@ -23,6 +23,7 @@
 //
 // A row whose scores pass its reference by more than fp32's range within one block, or whose masked keys hold NaN or Inf
 // values (weight 0, but 0 x Inf is not 0), comes out non-finite and is computed again from the keys that it sees, by a warp.
+// So is one whose weights sum to next to nothing (scores of 2^30 and more, see there).
 #include <algorithm>
 #include <type_traits>
 
