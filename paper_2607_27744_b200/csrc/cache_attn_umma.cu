@@ -779,10 +779,10 @@ umma_kernel(const __grid_constant__ CUtensorMap map_q, const __grid_constant__ C
       if (leads) {
         bad = there && (split ? ends[0].z + ends[kSide].z + ends[2 * kSide].z + ends[3 * kSide].z
                               : ends[side * 2 * kSide].z + ends[(side * 2 + 1) * kSide].z) != 0.f;
+        bad = bad || (there && beyond);
         // Scores of 2^30 and more: their product with the scale is not rounded where the reference was, so that the largest weight
         // may have come out as 2^-64 and less, beside others that 2^-126 or exp2_pair's least cut off.  (Without a reference it may
         // be 2^-80.)
-        bad = bad || (there && beyond);
         bad = bad || (sees && l_all < (bounded ? 0x1p-100f : 0x1p-64f) && keys.lo < (blk0 + n) * BK && keys.hi > blk0 * BK);
       }
       uint32_t redo = __ballot_sync(0xffffffffu, bad);
